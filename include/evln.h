@@ -416,6 +416,94 @@ evlnStatus_t evlnStoreFetch(evlnHandle_t handle, const evlnGatherParams* params,
                             const void* h_v_store, int host_capacity, int src_slot, int len, void* k_store,
                             void* v_store, int dst_slot, void* stream);
 
+/* ---- norms of queries and keys (no counterpart in the paper; models whose attention normalises each head's
+ *      queries and keys before the rotation) -----------------------------------------------------------------
+ *
+ * evlnRopeAppend / evlnPagedRopeAppend with a norm of every query and key head in the same pass:
+ *     y = w * x / sqrt(mean(x^2) + eps)        mean over the D channels of the head,
+ * then the rotation, then the stores.  Sums are fp32, and there is one rounding, to the storage type, after the rotation
+ * (none between norm and rotation).  Values are copied.  A head of zeros with eps = 0 gives NaN, as the formula does.
+ * A model whose weights are stored as w - 1 passes 1 + them.  The paged call takes token strides, as the contiguous one
+ * does, so that q, k and v may be views of one projection's rows.                                        */
+typedef struct {
+    size_t struct_size;      /* sizeof(evlnHeadNorm)                                         */
+    const void* q_weight;    /* [D], the tokens' type, 16-byte aligned; NULL: ones           */
+    const void* k_weight;
+    float eps;               /* >= 0                                                         */
+} evlnHeadNorm;
+
+evlnStatus_t evlnNormRopeAppend(evlnHandle_t handle, const evlnStepParams* params, const evlnHeadNorm* norm,
+                                const void* q_new, const void* k_new, const void* v_new,
+                                long q_stride_tok, long k_stride_tok, long v_stride_tok,
+                                void* q_rot, void* k_cache, void* v_cache, void* stream);
+evlnStatus_t evlnPagedNormRopeAppend(evlnHandle_t handle, const evlnPagedParams* params, const evlnHeadNorm* norm,
+                                     const void* q_new, const void* k_new, const void* v_new,
+                                     long q_stride_tok, long k_stride_tok, long v_stride_tok,
+                                     const int* h_cache_lens, const int* h_new_offsets, const int* d_page_table,
+                                     void* q_rot, void* k_pool, void* v_pool, void* stream);
+
+/* ---- paged cache in 8 bits (no counterpart in the paper: half the bytes of the cache, so twice the episodes on a GPU
+ *      and half the time of a step that is bound by reading it) --------------------------------------------------
+ *
+ * k_pool, v_pool [num_pages, Hkv, 64, 128] hold codes of one byte (e4m3: 4 exponent, 3 fraction bits, largest 448,
+ * no infinities, NaN 0x7f / 0xff), k_scale, v_scale [num_pages, Hkv] a float for each page and kv head:
+ *     value = code * scale.
+ * Lengths, offsets and page tables are those of the evlnPaged* calls (evlnPagedCheckTable serves them too), and so
+ * are the limits: bf16 queries, keys, values and output, head_dim 128, pages of 64 tokens.
+ *
+ * evlnPaged8RopeAppend: evlnPagedRopeAppend (norm = NULL) or evlnPagedNormRopeAppend into such a cache.  Queries go to
+ * q_rot in bf16.  Keys (after the rotation, in fp32) and values are rounded to the nearest code, ties to even, with
+ *     scale = the least power of two, 2^-120 .. 2^120, with |x| <= 448 scale for every new x of the page and head.
+ * A page that held earlier tokens of the episode keeps its scale if that is larger; if it is smaller the page takes the
+ * new scale and the earlier codes are rounded anew (exact while they stay normal numbers).  Infinities are stored as
+ * the largest code, NaN as NaN, and neither counts for the scale.  Value slots behind the episode's last token are
+ * cleared up to the end of its page; key slots there, and pages that no new token goes to, are left as they were.
+ *
+ * evlnPaged8StepAttention: causal attention of the rotated queries over such a cache, out and lse_out (may be NULL) as
+ * from evlnPagedStepAttention + evlnPagedStepCombine.  Up to a few hundred query rows per kv head are read from the codes
+ * themselves, more are served from a bf16 copy of the batch's pages in the workspace (exact: code * scale is a bf16
+ * number), so that evlnPaged8WorkspaceSize is larger for those.                                            */
+evlnStatus_t evlnPaged8RopeAppend(evlnHandle_t handle, const evlnPagedParams* params, const evlnHeadNorm* norm,
+                                  const void* q_new, const void* k_new, const void* v_new,
+                                  long q_stride_tok, long k_stride_tok, long v_stride_tok,
+                                  const int* h_cache_lens, const int* h_new_offsets, const int* d_page_table,
+                                  void* q_rot, void* k_pool, void* v_pool, float* k_scale, float* v_scale, void* stream);
+evlnStatus_t evlnPaged8WorkspaceSize(evlnHandle_t handle, const evlnPagedParams* params, const int* h_cache_lens,
+                                     const int* h_new_offsets, size_t* bytes);
+evlnStatus_t evlnPaged8StepAttention(evlnHandle_t handle, const evlnPagedParams* params, const void* q_rot,
+                                     const void* k_pool, const void* v_pool, const float* k_scale, const float* v_scale,
+                                     const int* h_cache_lens, const int* h_new_offsets, const int* d_page_table,
+                                     void* workspace, size_t workspace_bytes, void* out, float* lse_out, void* stream);
+
+/* ---- eviction by accumulated attention weight (Sec. 3.2 keeps frames by uniform or sliding-window sampling; this is a
+ *      sampler by what the queries have attended to, token by token and kv head by kv head) --------------------
+ *
+ * evlnKeyWeights: what a step's queries gave each key, added up over the query heads of a kv head,
+ *     weights_out[g][j] = decay * weights_in[g][j] (j < L)  +  sum over rows i, h of group g that see key j of
+ *                         exp(softmax_scale q_ih . k_j - lse_ih),                                j = 0 .. L+n-1.
+ * q_rot and k_cache as evlnRopeAppend leaves them, lse [n, Hq] as the step's combine writes it, params those of the step.
+ * weights_in, weights_out float [Hkv, cache_capacity] (the same buffer, or two that do not overlap); slots from L+n on are not
+ * touched, and weights_in is not read from slot L on.  decay >= 0.  bf16 and f32, head_dim 64 and 128.  num_splits
+ * and kernel of params are not looked at.  Results do not depend on timing (no atomics).
+ *
+ * evlnSelectKeys: for each kv head the slots to keep of 0 .. num_keys-1: all of them where budget >= num_keys, else the first
+ * `sinks`, the last `recent` and of those between the budget - sinks - recent of largest weight (equal weights: the
+ * lower slot; NaN counts as less than any number).  kept [Hkv, min(budget, num_keys)] int, ascending.  weights
+ * float [Hkv, store_capacity].  sinks + recent <= budget.
+ *
+ * evlnGatherKeys: the chosen slots of the store laid out back to back, kv head by kv head: key and value kept[g][p] of head g
+ * go to working slot p, the key turned by the rotation of position p (rotate != 0: the store is un-rotated) or copied
+ * as it is (rotate = 0: a cache whose keys keep the positions that they have).  Values, and weights where both weight
+ * buffers are given ([Hkv, store_capacity], [Hkv, work_capacity]), are copied.  The working buffers must not overlap the store.
+ * An entry of `kept` outside 0 .. store_capacity-1 gives zeros.  Slots from num_kept on are not touched.     */
+evlnStatus_t evlnKeyWeights(evlnHandle_t handle, const evlnStepParams* params, const void* q_rot, const void* k_cache,
+                            const float* lse, float decay, const float* weights_in, float* weights_out, void* stream);
+evlnStatus_t evlnSelectKeys(evlnHandle_t handle, const evlnGatherParams* params, const float* weights, int num_keys,
+                            int budget, int sinks, int recent, int* kept, void* stream);
+evlnStatus_t evlnGatherKeys(evlnHandle_t handle, const evlnGatherParams* params, int num_kept, const int* kept,
+                            const float* weights, const void* k_store, const void* v_store, float* weights_work,
+                            void* k_work, void* v_work, int rotate, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,8 +27,12 @@ def native_path() -> str:
 
 
 NATIVE_PATH = native_path()
-_SOURCES = ["evln_api.cu", "attn_pair.cuh", "attn_few.cuh", "attn_simt.cuh", "attn_f32.cuh", "attn_f32_small.cuh", "combine.cuh", "rope_append.cuh",
-            "common.cuh", "ptx_sm100.cuh", "gather_rope.cuh", "timeline_debug.cuh"]
+_UNITS = {        # translation units and the headers that they include
+    "evln_api.cu": ["attn_pair.cuh", "attn_few.cuh", "attn_simt.cuh", "attn_f32.cuh", "attn_f32_small.cuh", "combine.cuh", "rope_append.cuh", "gather_rope.cuh",
+                    "timeline_debug.cuh"],
+    "cache_ops.cu": ["attn8.cuh", "cache8.cuh", "evict.cuh", "head_norm.cuh", "key_weights.cuh"],
+}
+_SHARED_SOURCES = ["common.cuh", "context.cuh", "ptx_sm100.cuh", "rotation.cuh", "tc_common.cuh"]
 
 EVLN_OK, EVLN_INVALID_VALUE, EVLN_NOT_SUPPORTED, EVLN_CACHE_FULL = 0, 1, 2, 3
 EVLN_WORKSPACE_TOO_SMALL, EVLN_CUDA_ERROR, EVLN_DEVICE_TIMEOUT = 4, 5, 6
@@ -46,6 +50,8 @@ EXPORTS = [
     "evlnPackedWorkspaceSize", "evlnPackedForward",
     "evlnStepAttentionNoAlloc",
     "evlnSampleFrames", "evlnStoreAppend", "evlnGatherRope", "evlnStoreOffload", "evlnStoreFetch",
+    "evlnNormRopeAppend", "evlnPagedNormRopeAppend", "evlnPaged8RopeAppend", "evlnPaged8WorkspaceSize", "evlnPaged8StepAttention",
+    "evlnKeyWeights", "evlnSelectKeys", "evlnGatherKeys",
 ]
 EVLN_NOALLOC_SCRATCH_BYTES = 32 << 20
 EVLN_SELFTEST_STATUS_CODE = 8
@@ -80,6 +86,10 @@ class evlnGatherParams(Structure):
                 ("rope_table", c_void_p), ("rope_table_first_pos", c_int), ("rope_table_count", c_int)]
 
 
+class evlnHeadNorm(Structure):
+    _fields_ = [("struct_size", c_size_t), ("q_weight", c_void_p), ("k_weight", c_void_p), ("eps", c_float)]
+
+
 EVLN_SAMPLE_UNIFORM, EVLN_SAMPLE_SLIDING = 0, 1
 
 
@@ -93,28 +103,39 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     """Compile the CUDA sources into ``lib/libevln.so`` for sm_100a (in-tree)."""
     src_dir = os.path.join(_PKG, "csrc")
     header = os.path.join(_ROOT, "include", "evln.h")
-    srcs = [os.path.join(src_dir, s) for s in _SOURCES] + [header]
     os.makedirs(os.path.dirname(LIB_PATH), exist_ok=True)
 
     def fresh(path, sources):
         return not force and os.path.exists(path) and all(os.path.getmtime(path) >= os.path.getmtime(s) for s in sources)
 
-    if not fresh(LIB_PATH, srcs):
-        _build_cuda(src_dir, verbose)
+    _build_cuda(src_dir, header, fresh, verbose)
     native_src = os.path.join(src_dir, "py_native.cpp")
     if not fresh(NATIVE_PATH, [native_src, header]):
         _build_native(native_src)
     return LIB_PATH
 
 
-def _build_cuda(src_dir, verbose):
-    tmp = LIB_PATH + f".tmp{os.getpid()}"
-    cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-o", tmp, os.path.join(src_dir, "evln_api.cu")]
-    if verbose:
-        cmd.insert(1, "-Xptxas=-v")
-    subprocess.check_call(cmd)
-    os.replace(tmp, LIB_PATH)
+def _build_cuda(src_dir, header, fresh, verbose):
+    """Compiles the units that have changed, side by side, and links them."""
+    arch = ["-gencode", "arch=compute_100a,code=sm_100a"]
+    objects, running = [], []
+    for unit, headers in _UNITS.items():
+        obj = os.path.join(os.path.dirname(LIB_PATH), unit + ".o")
+        objects.append(obj)
+        if not fresh(obj, [os.path.join(src_dir, s) for s in [unit, *headers, *_SHARED_SOURCES]] + [header]):
+            tmp = obj + f".tmp{os.getpid()}.o"
+            cmd = ["nvcc", *(["-Xptxas=-v"] if verbose else []), *arch, "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-c", "-o", tmp,
+                   os.path.join(src_dir, unit)]
+            running.append((subprocess.Popen(cmd), tmp, obj))
+    failed = [process for process, _, _ in running if process.wait() != 0]
+    if failed:
+        raise subprocess.CalledProcessError(failed[0].returncode, failed[0].args)
+    for _, tmp, obj in running:
+        os.replace(tmp, obj)
+    if not fresh(LIB_PATH, objects):
+        tmp = LIB_PATH + f".tmp{os.getpid()}"
+        subprocess.check_call(["nvcc", *arch, "-shared", "-Xcompiler", "-fPIC", "-o", tmp, *objects])
+        os.replace(tmp, LIB_PATH)
 
 
 def _build_native(src):
@@ -189,6 +210,18 @@ def lib():
                                        c_void_p]
         L.evlnStoreFetch.argtypes = [c_void_p, qp, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p, c_int,
                                      c_void_p]
+        np = POINTER(evlnHeadNorm)
+        L.evlnNormRopeAppend.argtypes = [c_void_p, pp, np, c_void_p, c_void_p, c_void_p, c_long, c_long, c_long, c_void_p, c_void_p, c_void_p, c_void_p]
+        L.evlnPagedNormRopeAppend.argtypes = [c_void_p, gp, np, c_void_p, c_void_p, c_void_p, c_long, c_long, c_long, ip, ip, c_void_p, c_void_p, c_void_p,
+                                              c_void_p, c_void_p]
+        L.evlnPaged8RopeAppend.argtypes = [c_void_p, gp, np, c_void_p, c_void_p, c_void_p, c_long, c_long, c_long, ip, ip, c_void_p, c_void_p, c_void_p,
+                                           c_void_p, c_void_p, c_void_p, c_void_p]
+        L.evlnPaged8WorkspaceSize.argtypes = [c_void_p, gp, ip, ip, POINTER(c_size_t)]
+        L.evlnPaged8StepAttention.argtypes = [c_void_p, gp, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, ip, ip, c_void_p, c_void_p, c_size_t, c_void_p,
+                                              c_void_p, c_void_p]
+        L.evlnKeyWeights.argtypes = [c_void_p, pp, c_void_p, c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_void_p]
+        L.evlnSelectKeys.argtypes = [c_void_p, qp, c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_void_p]
+        L.evlnGatherKeys.argtypes = [c_void_p, qp, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p]
         for name in EXPORTS:
             if name not in ("evlnGetErrorString", "evlnRopeTableBytes"):
                 getattr(L, name).restype = c_int
@@ -336,6 +369,18 @@ def gather_params(dtype, num_kv_heads, head_dim, store_capacity, work_capacity, 
                             work_capacity, rope_theta, _ptr(rope_table), rope_table_first_pos, rope_table_count)
 
 
+def head_norm(q_weight=None, k_weight=None, eps=1e-6) -> evlnHeadNorm:
+    """``q_weight`` / ``k_weight``: ``[head_dim]`` tensors of the tokens' type (None: ones).  The structure holds their addresses
+    only: keep the tensors."""
+    return evlnHeadNorm(ctypes.sizeof(evlnHeadNorm), _ptr(q_weight), _ptr(k_weight), eps)
+
+
+def evlnPaged8WorkspaceSize(handle, params, cache_lens, new_offsets) -> int:
+    v = c_size_t(0)
+    _check(lib().evlnPaged8WorkspaceSize(handle, byref(params), _ints(cache_lens), _ints(new_offsets), byref(v)), "evlnPaged8WorkspaceSize")
+    return int(v.value)
+
+
 def evlnSampleFrames(sampler: int, num_frames: int, budget: int, stride: int = 1):
     """Host helper: indices of the history frames the sampler keeps (ascending)."""
     buf = (c_int * max(budget, 1))()
@@ -365,7 +410,8 @@ def evlnStoreFetch(handle, params, h_k_store, h_v_store, src_slot, length, k_sto
 # host time, twice what its three launches take, and more than the GPU needs for a step of a few tokens.
 kHotCalls = ("evlnRopeTable", "evlnRopeAppend", "evlnStepAttention", "evlnStepCombine", "evlnStep",
              "evlnPagedRopeAppend", "evlnPagedStepAttention", "evlnPagedStepCombine", "evlnPackedForward",
-             "evlnStepAttentionNoAlloc", "evlnStoreAppend", "evlnGatherRope")
+             "evlnStepAttentionNoAlloc", "evlnStoreAppend", "evlnGatherRope", "evlnNormRopeAppend", "evlnPagedNormRopeAppend",
+             "evlnPaged8RopeAppend", "evlnPaged8StepAttention", "evlnKeyWeights", "evlnSelectKeys", "evlnGatherKeys")
 
 
 def _load_native():
@@ -379,7 +425,7 @@ def _load_native():
     spec = importlib.util.spec_from_file_location("_evln_native", NATIVE_PATH)
     native = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(native)
-    native.configure(evlnStepParams, evlnPagedParams, evlnPackedParams, evlnGatherParams, EvlnError, ctypes.ArgumentError)
+    native.configure(evlnStepParams, evlnPagedParams, evlnPackedParams, evlnGatherParams, evlnHeadNorm, EvlnError, ctypes.ArgumentError)
     for name in kHotCalls:
         globals()[name] = getattr(native, name)
 

@@ -33,7 +33,6 @@ struct F32Fused {
 };
 
 constexpr int kSmallThreads = 256, kSmallRows = 32;
-constexpr int kSmallCluster = 16;                     // most splits of a one-launch step
 constexpr int kSmallAngleTokens = 80;                 // most tokens whose angles a block of a one-launch step holds
 
 template <int D> struct SmallPlan {

@@ -1,0 +1,473 @@
+// C-ABI entry points of the operators around the cache (contract: include/evln.h): norms of queries and keys with the append,
+// the cache in 8 bits, and eviction by attention weight.  Host-side checks, schedules and launches.
+#include "../../include/evln.h"
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <utility>
+
+#include "attn8.cuh"
+#include "cache8.cuh"
+#include "common.cuh"
+#include "context.cuh"
+#include "evict.cuh"
+#include "head_norm.cuh"
+#include "key_weights.cuh"
+
+using namespace evln;
+
+namespace evln {
+
+cudaError_t prepare_cache_kernels()
+{
+    const std::pair<const void*, int> kernels[] = {{(const void*)attn8_kernel<1, 1>, Attn8Plan<1, 1>::kBytes},
+                                                   {(const void*)attn8_kernel<2, 1>, Attn8Plan<2, 1>::kBytes},
+                                                   {(const void*)attn8_kernel<2, 2>, Attn8Plan<2, 2>::kBytes},
+                                                   {(const void*)key_weights_kernel<64>, KeyWeightPlan<64>::kBytes},
+                                                   {(const void*)key_weights_kernel<128>, KeyWeightPlan<128>::kBytes},
+                                                   {(const void*)select_keys_kernel, kSelectCache * 4}};
+    for (const auto& k : kernels) {
+        const cudaError_t e = cudaFuncSetAttribute(k.first, cudaFuncAttributeMaxDynamicSharedMemorySize, k.second);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace evln
+
+namespace {
+
+evlnStatus_t launched(evlnHandle_t h, cudaError_t e)
+{
+    return e == cudaSuccess ? EVLN_OK : cuda_fail(h, e);
+}
+
+// ---- norms with the append -------------------------------------------------------------------
+
+evlnStatus_t check_norm(const evlnHeadNorm* norm)
+{
+    if (!norm || norm->struct_size != sizeof(evlnHeadNorm) || !(norm->eps >= 0.f)) return EVLN_INVALID_VALUE;
+    if ((norm->q_weight && !aligned16(norm->q_weight)) || (norm->k_weight && !aligned16(norm->k_weight))) return EVLN_INVALID_VALUE;
+    return EVLN_OK;
+}
+
+// New tokens and where they go: pointers, alignment, strides (elements; vec: of a 16-byte vector).
+evlnStatus_t check_tokens(const void* const* pointers, int count, int hq, int hkv, int D, int vec, long qs, long ks, long vs)
+{
+    for (int i = 0; i < count; ++i)
+        if (!pointers[i] || !aligned16(pointers[i])) return EVLN_INVALID_VALUE;
+    if (qs < (long)hq * D || ks < (long)hkv * D || vs < (long)hkv * D) return EVLN_INVALID_VALUE;
+    if (qs % vec || ks % vec || vs % vec) return EVLN_INVALID_VALUE;
+    return EVLN_OK;
+}
+
+RopeArgs token_args(int hq, int hkv, int D, int vec, const void* q, const void* k, const void* v, long qs, long ks, long vs, double theta, const void* table,
+                    int table_first)
+{
+    RopeArgs a = {};
+    a.q_new = q; a.k_new = k; a.v_new = v;
+    a.q_stride = qs; a.k_stride = ks; a.v_stride = vs;
+    a.Hq = hq; a.Hkv = hkv; a.D = D;
+    a.log2_theta = log2(theta);
+    a.table = (const double2*)table;
+    a.table_first = table_first;
+    a.G = hq / hkv;
+    a.div_g = make_fast_div((uint32_t)a.G);
+    while ((1 << a.vph_shift) < D / 2 / vec) ++a.vph_shift;
+    return a;
+}
+
+NormArgs norm_args(const evlnHeadNorm* norm)
+{
+    NormArgs n = {};
+    if (norm) { n.q_weight = norm->q_weight; n.k_weight = norm->k_weight; n.eps = norm->eps; }
+    return n;
+}
+
+// A block per token with a thread per work item, as for the append without norms; few tokens of many heads get several.
+dim3 token_grid(int tokens, int extra, int items, dim3* block)
+{
+    const int parts = tokens <= kRopeFewTokens ? ceil_div(items, kRopeThreadsMax) : 1, t = (ceil_div(items, parts) + 31) / 32 * 32;
+    *block = dim3(t > kRopeThreadsMax ? kRopeThreadsMax : t < 64 ? 64 : t);
+    return dim3((unsigned)(tokens + extra), (unsigned)parts);
+}
+
+void batch_lens(BatchLens* bl, const evlnPagedParams* p, const int* lens, const int* offs)
+{
+    memset(bl, 0, sizeof(*bl));
+    for (int b = 0; b < p->batch; ++b) bl->cache_len[b] = lens[b];
+    for (int b = 0; b <= kMaxBatch; ++b) bl->new_off[b] = offs[b < p->batch ? b : p->batch];
+}
+
+// ---- attention over the cache in 8 bits ----------------------------------------------------------
+
+// Most query rows of an episode (per kv head) that the kernel on the codes serves; more go through a bf16 copy.
+constexpr int kA8MostRows = 256;
+
+struct Plan8 {
+    bool expand;
+    int rows;                // of a tile: 16, 32 or 64
+    int share, total, blocks;
+    int pages;               // expand: pages of the copy
+    size_t copy_bytes;       // expand: table and pools
+};
+
+template <typename F>
+void for_episodes(const evlnPagedParams* p, const int* lens, const int* offs, F&& f)
+{
+    for (int b = 0; b < p->batch; ++b) f(b, lens[b], offs[b + 1] - offs[b]);
+}
+
+evlnStatus_t plan8(evlnHandle_t h, const evlnPagedParams* p, const int* lens, const int* offs, Plan8* pl)
+{
+    const int G = p->num_q_heads / p->num_kv_heads;
+    long most = 0, total = 0, pages = 0;
+    for_episodes(p, lens, offs, [&](int, int, int n) { if ((long)n * G > most) most = (long)n * G; });
+    *pl = Plan8();
+    pl->expand = most > kA8MostRows;
+    pl->rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+    for_episodes(p, lens, offs, [&](int, int L, int n) {
+        if (n == 0) return;
+        pages += ((long)L + n + kPage8 - 1) / kPage8;
+        total += ((long)n * G + pl->rows - 1) / pl->rows * p->num_kv_heads * (((long)L + n + kA8Keys - 1) / kA8Keys);
+    });
+    if (total > 0x3fffffffL || pages > 0x3fffffffL) return EVLN_NOT_SUPPORTED;
+    if (pl->expand) {
+        pl->pages = (int)pages;
+        pl->copy_bytes = round_up((size_t)p->batch * p->max_pages_per_seq * sizeof(int), 1024) + (size_t)pages * p->num_kv_heads * kPage8 * 128 * 2 * 2;
+        return EVLN_OK;
+    }
+    // an SM each, but at least a stage for every warp of a block
+    pl->total = (int)total;
+    pl->share = ceil_div(pl->total, h->num_sms);
+    if (pl->share < kA8Warps) pl->share = kA8Warps;
+    pl->blocks = ceil_div(pl->total, pl->share);
+    return EVLN_OK;
+}
+
+size_t part_bytes8(const Plan8& pl) { return round_up((size_t)2 * pl.blocks * pl.rows * (128 + 1) * sizeof(float), 256); }
+
+// The paged call that serves the bf16 copy.
+evlnPagedParams copy_params(const evlnPagedParams* p, const Plan8& pl)
+{
+    evlnPagedParams c = *p;
+    c.num_pages = pl.pages;
+    return c;
+}
+
+template <int MT, int RG>
+cudaError_t launch_attn8(const Plan8& pl, cudaStream_t st, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Attn8Args& a, const BatchLens& bl)
+{
+    using Plan = Attn8Plan<MT, RG>;
+    cudaError_t e = launch_pdl(attn8_kernel<MT, RG>, dim3(pl.blocks), dim3(kA8Threads), Plan::kBytes, st, tm_k, tm_v, a, bl);
+    if (e == cudaSuccess && pl.blocks > 1)
+        e = launch_pdl(merge8_kernel<Plan::kRows>, dim3(pl.blocks - 1, Plan::kRows / 4), dim3(128), 0, st, a, bl);
+    return e;
+}
+
+}  // namespace
+
+extern "C" {
+
+evlnStatus_t evlnNormRopeAppend(evlnHandle_t h, const evlnStepParams* p, const evlnHeadNorm* norm, const void* q_new, const void* k_new,
+                                const void* v_new, long q_stride_tok, long k_stride_tok, long v_stride_tok, void* q_rot, void* k_cache,
+                                void* v_cache, void* stream)
+{
+    evlnStatus_t s = check_step_params(h, p);
+    if (s == EVLN_OK) s = check_norm(norm);
+    if (s != EVLN_OK) return s;
+    if (p->num_new == 0) return EVLN_OK;
+    const int vec = 16 / elem_bytes(p->dtype);
+    const void* pointers[6] = {q_new, k_new, v_new, q_rot, k_cache, v_cache};
+    s = check_tokens(pointers, 6, p->num_q_heads, p->num_kv_heads, p->head_dim, vec, q_stride_tok, k_stride_tok, v_stride_tok);
+    if (s != EVLN_OK) return s;
+    if (!device_is_current(h)) return EVLN_INVALID_VALUE;
+    RopeArgs a = token_args(p->num_q_heads, p->num_kv_heads, p->head_dim, vec, q_new, k_new, v_new, q_stride_tok, k_stride_tok, v_stride_tok, p->rope_theta,
+                            p->rope_table, p->rope_table_first_pos);
+    a.q_rot = q_rot; a.k_cache = k_cache; a.v_cache = v_cache;
+    a.cache_len = p->cache_len; a.num_new = p->num_new; a.cache_cap = p->cache_capacity;
+    dim3 block;
+    const dim3 grid = token_grid(p->num_new, 0, ((a.Hq + a.Hkv) << a.vph_shift) + (a.Hkv << (a.vph_shift + 1)), &block);
+    const NoLens nl = {};
+    const NormArgs n = norm_args(norm);
+    return launched(h, p->dtype == EVLN_BF16 ? launch_pdl(norm_append_kernel<__nv_bfloat16, false, NoLens>, grid, block, 0, (cudaStream_t)stream, a, n, nl)
+                                             : launch_pdl(norm_append_kernel<float, false, NoLens>, grid, block, 0, (cudaStream_t)stream, a, n, nl));
+}
+
+evlnStatus_t evlnPagedNormRopeAppend(evlnHandle_t h, const evlnPagedParams* p, const evlnHeadNorm* norm, const void* q_new, const void* k_new,
+                                     const void* v_new, long q_stride_tok, long k_stride_tok, long v_stride_tok, const int* h_cache_lens,
+                                     const int* h_new_offsets, const int* d_page_table, void* q_rot, void* k_pool, void* v_pool, void* stream)
+{
+    evlnStatus_t s = check_paged_params(h, p, h_cache_lens, h_new_offsets);
+    if (s == EVLN_OK) s = check_norm(norm);
+    if (s != EVLN_OK) return s;
+    const int total = h_new_offsets[p->batch];
+    if (total == 0) return EVLN_OK;
+    const void* pointers[6] = {q_new, k_new, v_new, q_rot, k_pool, v_pool};
+    s = check_tokens(pointers, 6, p->num_q_heads, p->num_kv_heads, 128, 8, q_stride_tok, k_stride_tok, v_stride_tok);
+    if (s != EVLN_OK) return s;
+    if (!d_page_table || !device_is_current(h)) return EVLN_INVALID_VALUE;
+    RopeArgs a = token_args(p->num_q_heads, p->num_kv_heads, 128, 8, q_new, k_new, v_new, q_stride_tok, k_stride_tok, v_stride_tok, p->rope_theta, p->rope_table,
+                            p->rope_table_first_pos);
+    a.q_rot = q_rot; a.k_cache = k_pool; a.v_cache = v_pool; a.page_table = d_page_table;
+    a.num_new = total; a.batch = p->batch; a.page_size = p->page_size; a.max_pages = p->max_pages_per_seq;
+    while ((1 << a.page_shift) < a.page_size) ++a.page_shift;
+    BatchLens bl;
+    batch_lens(&bl, p, h_cache_lens, h_new_offsets);
+    dim3 block;
+    const dim3 grid = token_grid(total, p->batch, ((a.Hq + a.Hkv) << a.vph_shift) + (a.Hkv << (a.vph_shift + 1)), &block);
+    return launched(h, launch_pdl(norm_append_kernel<__nv_bfloat16, true, BatchLens>, grid, block, 0, (cudaStream_t)stream, a, norm_args(norm), bl));
+}
+
+evlnStatus_t evlnPaged8RopeAppend(evlnHandle_t h, const evlnPagedParams* p, const evlnHeadNorm* norm, const void* q_new, const void* k_new,
+                                  const void* v_new, long q_stride_tok, long k_stride_tok, long v_stride_tok, const int* h_cache_lens,
+                                  const int* h_new_offsets, const int* d_page_table, void* q_rot, void* k_pool, void* v_pool, float* k_scale,
+                                  float* v_scale, void* stream)
+{
+    evlnStatus_t s = check_paged_params(h, p, h_cache_lens, h_new_offsets);
+    if (s == EVLN_OK && norm) s = check_norm(norm);
+    if (s != EVLN_OK) return s;
+    const int total = h_new_offsets[p->batch];
+    if (total == 0) return EVLN_OK;
+    const void* pointers[6] = {q_new, k_new, v_new, q_rot, k_pool, v_pool};
+    s = check_tokens(pointers, 6, p->num_q_heads, p->num_kv_heads, 128, 8, q_stride_tok, k_stride_tok, v_stride_tok);
+    if (s != EVLN_OK) return s;
+    if (!d_page_table || !k_scale || !v_scale || !device_is_current(h)) return EVLN_INVALID_VALUE;
+    Append8Args a = {};
+    a.r = token_args(p->num_q_heads, p->num_kv_heads, 128, 8, q_new, k_new, v_new, q_stride_tok, k_stride_tok, v_stride_tok, p->rope_theta, p->rope_table,
+                     p->rope_table_first_pos);
+    a.r.q_rot = q_rot; a.r.k_cache = k_pool; a.r.v_cache = v_pool; a.r.page_table = d_page_table;
+    a.r.num_new = total; a.r.batch = p->batch; a.r.page_size = kPage8; a.r.max_pages = p->max_pages_per_seq;
+    a.norm = norm_args(norm);
+    a.k_scale = k_scale; a.v_scale = v_scale;
+    BatchLens bl;
+    batch_lens(&bl, p, h_cache_lens, h_new_offsets);
+    long pages = 0;
+    for (int b = 0; b <= kMaxBatch; ++b) {
+        bl.item_off[b] = (int)pages;
+        if (b >= p->batch) continue;
+        const int L = h_cache_lens[b], n = h_new_offsets[b + 1] - h_new_offsets[b];
+        if (n > 0) pages += ((long)L + n + kPage8 - 1) / kPage8 - L / kPage8;
+    }
+    // queries: a block per 256 work items of a token where there are few tokens, else one per token
+    a.q_parts = total <= kRopeFewTokens ? ceil_div(a.r.Hq << a.r.vph_shift, kAppend8Threads) : 1;
+    const long blocks = 2 * pages * p->num_kv_heads + (long)total * a.q_parts;
+    if (blocks > 0x3fffffffL) return EVLN_NOT_SUPPORTED;
+    a.page_blocks = (int)(pages * p->num_kv_heads);
+    a.div_hkv = make_fast_div((uint32_t)p->num_kv_heads);
+    a.div_parts = make_fast_div((uint32_t)a.q_parts);
+    return launched(h, norm ? launch_pdl(append8_kernel<true>, dim3((unsigned)blocks), dim3(kAppend8Threads), 0, (cudaStream_t)stream, a, bl)
+                            : launch_pdl(append8_kernel<false>, dim3((unsigned)blocks), dim3(kAppend8Threads), 0, (cudaStream_t)stream, a, bl));
+}
+
+evlnStatus_t evlnPaged8WorkspaceSize(evlnHandle_t h, const evlnPagedParams* p, const int* h_cache_lens, const int* h_new_offsets, size_t* bytes)
+{
+    evlnStatus_t s = check_paged_params(h, p, h_cache_lens, h_new_offsets);
+    if (s != EVLN_OK) return s;
+    if (!bytes) return EVLN_INVALID_VALUE;
+    Plan8 pl;
+    s = plan8(h, p, h_cache_lens, h_new_offsets, &pl);
+    if (s != EVLN_OK) return s;
+    if (!pl.expand) {
+        *bytes = part_bytes8(pl);
+        return EVLN_OK;
+    }
+    const evlnPagedParams c = copy_params(p, pl);
+    size_t inner = 0;
+    s = evlnPagedWorkspaceSize(h, &c, h_cache_lens, h_new_offsets, &inner);
+    *bytes = pl.copy_bytes + inner;
+    return s;
+}
+
+evlnStatus_t evlnPaged8StepAttention(evlnHandle_t h, const evlnPagedParams* p, const void* q_rot, const void* k_pool, const void* v_pool,
+                                     const float* k_scale, const float* v_scale, const int* h_cache_lens, const int* h_new_offsets,
+                                     const int* d_page_table, void* workspace, size_t workspace_bytes, void* out, float* lse_out, void* stream)
+{
+    size_t need = 0;
+    evlnStatus_t s = evlnPaged8WorkspaceSize(h, p, h_cache_lens, h_new_offsets, &need);
+    if (s != EVLN_OK) return s;
+    const int total = h_new_offsets[p->batch];
+    if (total == 0) return EVLN_OK;
+    const void* pointers[5] = {q_rot, k_pool, v_pool, workspace, out};
+    for (const void* x : pointers)
+        if (!x || !aligned16(x)) return EVLN_INVALID_VALUE;
+    if (!k_scale || !v_scale || !d_page_table || !device_is_current(h)) return EVLN_INVALID_VALUE;
+    if (workspace_bytes < need) return EVLN_WORKSPACE_TOO_SMALL;
+    Plan8 pl;
+    s = plan8(h, p, h_cache_lens, h_new_offsets, &pl);
+    if (s != EVLN_OK) return s;
+    cudaStream_t st = (cudaStream_t)stream;
+    const int G = p->num_q_heads / p->num_kv_heads, hkv = p->num_kv_heads;
+    BatchLens bl;
+    batch_lens(&bl, p, h_cache_lens, h_new_offsets);
+
+    if (pl.expand) {
+        const evlnPagedParams c = copy_params(p, pl);
+        int at = 0;
+        for (int b = 0; b <= kMaxBatch; ++b) {
+            bl.item_off[b] = at;
+            if (b < p->batch && h_new_offsets[b + 1] > h_new_offsets[b]) at += ceil_div(h_cache_lens[b] + h_new_offsets[b + 1] - h_new_offsets[b], kPage8);
+        }
+        Expand8Args a = {};
+        a.k_pool = (const uint8_t*)k_pool; a.v_pool = (const uint8_t*)v_pool;
+        a.k_scale = k_scale; a.v_scale = v_scale;
+        a.page_table = d_page_table;
+        a.out_table = (int*)workspace;
+        a.k_out = (__nv_bfloat16*)((char*)workspace + round_up((size_t)p->batch * p->max_pages_per_seq * sizeof(int), 1024));
+        a.v_out = a.k_out + (size_t)pl.pages * hkv * kPage8 * 128;
+        a.Hkv = hkv; a.batch = p->batch; a.max_pages = p->max_pages_per_seq;
+        void* inner = (char*)workspace + pl.copy_bytes;
+        s = launched(h, launch_pdl(expand8_kernel, dim3((unsigned)pl.pages, (unsigned)hkv, 2), dim3(256), 0, st, a, bl));
+        if (s == EVLN_OK)
+            s = evlnPagedStepAttention(h, &c, q_rot, a.k_out, a.v_out, h_cache_lens, h_new_offsets, a.out_table, inner, workspace_bytes - pl.copy_bytes, stream);
+        if (s == EVLN_OK) s = evlnPagedStepCombine(h, &c, inner, h_cache_lens, h_new_offsets, out, lse_out, stream);
+        return s;
+    }
+
+    int at = 0;
+    for (int b = 0; b <= kMaxBatch; ++b) {
+        bl.item_off[b] = at;
+        if (b >= p->batch) continue;
+        const int L = h_cache_lens[b], n = h_new_offsets[b + 1] - h_new_offsets[b];
+        if (n > 0) at += ceil_div(n * G, pl.rows) * hkv * ceil_div(L + n, kA8Keys);
+    }
+    CUtensorMap tm_k, tm_v;
+    const cuuint64_t dims[2] = {128, (cuuint64_t)p->num_pages * hkv * kPage8}, strides[1] = {128};
+    const cuuint32_t box[2] = {128, kA8Keys};
+    if (dims[1] > 0x7fffffffULL) return EVLN_NOT_SUPPORTED;
+    if (!encode_map(h, &tm_k, k_pool, 2, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8)) return EVLN_INVALID_VALUE;
+    if (!encode_map(h, &tm_v, v_pool, 2, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8)) return EVLN_INVALID_VALUE;
+    Attn8Args a = {};
+    a.q_rot = (const __nv_bfloat16*)q_rot;
+    a.k_scale = k_scale; a.v_scale = v_scale;
+    a.page_table = d_page_table;
+    a.out = (__nv_bfloat16*)out; a.lse_out = lse_out;
+    a.o_part = (float*)workspace;
+    a.lse_part = a.o_part + (size_t)2 * pl.blocks * pl.rows * 128;
+    a.status = h->d_status;
+    a.Hkv = hkv; a.G = G; a.rows = total * G; a.batch = p->batch; a.max_pages = p->max_pages_per_seq;
+    a.share = pl.share; a.total = pl.total;
+    a.scale_log2 = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf(128.f)) * 1.4426950408889634f;
+    a.div_g = make_fast_div((uint32_t)G);
+    return launched(h, pl.rows == 16   ? launch_attn8<1, 1>(pl, st, tm_k, tm_v, a, bl)
+                       : pl.rows == 32 ? launch_attn8<2, 1>(pl, st, tm_k, tm_v, a, bl)
+                                       : launch_attn8<2, 2>(pl, st, tm_k, tm_v, a, bl));
+}
+
+// ---- eviction --------------------------------------------------------------------------------
+
+evlnStatus_t evlnKeyWeights(evlnHandle_t h, const evlnStepParams* p, const void* q_rot, const void* k_cache, const float* lse, float decay,
+                            const float* weights_in, float* weights_out, void* stream)
+{
+    evlnStatus_t s = check_step_params(h, p);
+    if (s != EVLN_OK) return s;
+    if (!(decay >= 0.f)) return EVLN_INVALID_VALUE;
+    if (p->num_new == 0) return EVLN_INVALID_VALUE;
+    if (!q_rot || !k_cache || !lse || !weights_in || !weights_out || !aligned16(q_rot) || !aligned16(k_cache)) return EVLN_INVALID_VALUE;
+    const size_t w_bytes = (size_t)p->num_kv_heads * p->cache_capacity * sizeof(float);
+    if (weights_in != weights_out && overlap(weights_in, w_bytes, weights_out, w_bytes)) return EVLN_INVALID_VALUE;
+    if (!device_is_current(h)) return EVLN_INVALID_VALUE;
+    const int D = p->head_dim, total = p->cache_len + p->num_new;
+    const long tiles = ((long)total + kTileN - 1) / kTileN;
+    if (tiles * p->num_kv_heads > 0x3fffffffL) return EVLN_NOT_SUPPORTED;
+    KeyWeightArgs a = {};
+    a.lse = lse; a.in = weights_in; a.out = weights_out;
+    a.q_rot = q_rot; a.k_cache = k_cache;
+    a.status = h->d_status;
+    a.Hkv = p->num_kv_heads; a.G = p->num_q_heads / p->num_kv_heads; a.rows = p->num_new * a.G;
+    a.L = p->cache_len; a.n = p->num_new; a.cap = p->cache_capacity;
+    a.items = (int)tiles * p->num_kv_heads;
+    a.scale_log2 = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
+    a.decay = decay;
+    a.div_g = make_fast_div((uint32_t)a.G);
+    a.div_hkv = make_fast_div((uint32_t)a.Hkv);
+    const bool f32 = p->dtype == EVLN_F32;
+    a.chunk_rows = f32 ? kKwF32Rows : a.rows >= 128 ? 128 : (a.rows + 31) / 32 * 32;
+    a.chunks = ceil_div(a.rows, a.chunk_rows);
+    // few tiles: a cluster of CTAs for each, as many as the SMs (fp32: four blocks an SM) and the chunks allow
+    int cluster = 1;
+    while (cluster < kKwMaxCluster && 2 * cluster <= a.chunks && 2L * cluster * a.items <= (f32 ? 4L : 1L) * h->num_sms) cluster *= 2;
+    const bool whole = cluster > 1 || f32;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(whole || a.items < h->num_sms ? a.items : h->num_sms), (unsigned)cluster);
+    cfg.blockDim = dim3(f32 ? kKwF32Keys : kKwThreads);
+    cfg.stream = (cudaStream_t)stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 1;
+    attr[1].val.clusterDim.y = (unsigned)cluster;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    if (f32) return launched(h, D == 128 ? cudaLaunchKernelEx(&cfg, key_weights_f32_kernel<128>, a) : cudaLaunchKernelEx(&cfg, key_weights_f32_kernel<64>, a));
+    CUtensorMap tm_k, tm_q;
+    const cuuint64_t kdims[3] = {(cuuint64_t)D, (cuuint64_t)p->cache_capacity, (cuuint64_t)p->num_kv_heads};
+    const cuuint64_t kstrides[2] = {(cuuint64_t)D * 2, (cuuint64_t)p->cache_capacity * D * 2};
+    const cuuint64_t qdims[3] = {(cuuint64_t)D, (cuuint64_t)a.rows, (cuuint64_t)p->num_kv_heads};
+    const cuuint64_t qstrides[2] = {(cuuint64_t)D * 2, (cuuint64_t)a.rows * D * 2};
+    const cuuint32_t kbox[3] = {64, kTileN, 1}, qbox[3] = {64, (cuuint32_t)a.chunk_rows, 1};
+    if (!encode_map(h, &tm_k, k_cache, 3, kdims, kstrides, kbox)) return EVLN_INVALID_VALUE;
+    if (!encode_map(h, &tm_q, q_rot, 3, qdims, qstrides, qbox)) return EVLN_INVALID_VALUE;
+    cfg.dynamicSmemBytes = D == 128 ? KeyWeightPlan<128>::kBytes : KeyWeightPlan<64>::kBytes;
+    return launched(h, D == 128 ? cudaLaunchKernelEx(&cfg, key_weights_kernel<128>, tm_k, tm_q, a) : cudaLaunchKernelEx(&cfg, key_weights_kernel<64>, tm_k, tm_q, a));
+}
+
+evlnStatus_t evlnSelectKeys(evlnHandle_t h, const evlnGatherParams* p, const float* weights, int num_keys, int budget, int sinks, int recent,
+                            int* kept, void* stream)
+{
+    evlnStatus_t s = check_gather_params(h, p);
+    if (s != EVLN_OK) return s;
+    if (num_keys < 0 || num_keys > p->store_capacity || budget < 0 || sinks < 0 || recent < 0 || (long)sinks + recent > budget) return EVLN_INVALID_VALUE;
+    SelectArgs a = {};
+    a.num_kept = budget < num_keys ? budget : num_keys;
+    if (a.num_kept == 0) return EVLN_OK;
+    if (!weights || !kept) return EVLN_INVALID_VALUE;
+    a.weights = weights; a.kept = kept;
+    a.stride = p->store_capacity; a.num_keys = num_keys;
+    a.sinks = sinks; a.recent = recent; a.open = budget - sinks - recent;
+    if (a.num_kept == num_keys) a.sinks = a.recent = a.open = 0;
+    a.cached = num_keys <= kSelectCache;
+    return launched(h, launch_pdl(select_keys_kernel, dim3((unsigned)p->num_kv_heads), dim3(kSelectThreads), a.cached ? (size_t)num_keys * 4 : 0, (cudaStream_t)stream, a));
+}
+
+evlnStatus_t evlnGatherKeys(evlnHandle_t h, const evlnGatherParams* p, int num_kept, const int* kept, const float* weights, const void* k_store,
+                            const void* v_store, float* weights_work, void* k_work, void* v_work, int rotate, void* stream)
+{
+    evlnStatus_t s = check_gather_params(h, p);
+    if (s != EVLN_OK) return s;
+    if (num_kept < 0) return EVLN_INVALID_VALUE;
+    if (num_kept > p->work_capacity) return EVLN_CACHE_FULL;
+    if (num_kept == 0) return EVLN_OK;
+    const void* pointers[4] = {k_store, v_store, k_work, v_work};
+    for (const void* x : pointers)
+        if (!x || !aligned16(x)) return EVLN_INVALID_VALUE;
+    if (!kept || (weights == nullptr) != (weights_work == nullptr)) return EVLN_INVALID_VALUE;
+    if (rotate && !rope_table_covers(p->rope_table, p->rope_table_first_pos, p->rope_table_count, 0, num_kept)) return EVLN_INVALID_VALUE;
+    const size_t row = (size_t)p->num_kv_heads * p->head_dim * elem_bytes(p->dtype), src = row * p->store_capacity, dst = row * p->work_capacity;
+    for (int i = 0; i < 2; ++i)
+        for (int j = 2; j < 4; ++j)
+            if (overlap(pointers[i], src, pointers[j], dst)) return EVLN_INVALID_VALUE;
+    if (weights && overlap(weights, (size_t)p->num_kv_heads * p->store_capacity * 4, weights_work, (size_t)p->num_kv_heads * p->work_capacity * 4)) return EVLN_INVALID_VALUE;
+    GatherKeysArgs a = {};
+    a.k_src = k_store; a.v_src = v_store; a.w_src = weights;
+    a.k_dst = k_work; a.v_dst = v_work; a.w_dst = weights_work;
+    a.kept = kept;
+    a.Hkv = p->num_kv_heads; a.D = p->head_dim; a.src_cap = p->store_capacity; a.dst_cap = p->work_capacity;
+    a.num_kept = num_kept; a.rotate = rotate != 0;
+    a.log2_theta = log2(p->rope_theta);
+    a.table = (const double2*)p->rope_table;
+    a.table_first = p->rope_table_first_pos;
+    const int vec = 16 / elem_bytes(p->dtype);
+    while ((1 << a.vph_shift) < a.D / 2 / vec) ++a.vph_shift;
+    const dim3 grid((unsigned)ceil_div(num_kept, kGatherKeysThreads / (a.D / 2))), block(kGatherKeysThreads);
+    return launched(h, p->dtype == EVLN_BF16 ? launch_pdl(gather_keys_kernel<__nv_bfloat16>, grid, block, 0, (cudaStream_t)stream, a)
+                                             : launch_pdl(gather_keys_kernel<float>, grid, block, 0, (cudaStream_t)stream, a));
+}
+
+}  // extern "C"

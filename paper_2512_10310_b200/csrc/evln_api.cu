@@ -22,24 +22,10 @@
 #include "combine.cuh"
 #include "gather_rope.cuh"
 #include "common.cuh"
+#include "context.cuh"
 #include "rope_append.cuh"
 
 using namespace evln;
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                  const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-struct evlnContext {
-    int device;
-    int num_sms;
-    int last_cuda_error;
-    int* d_status;
-    EncodeTiledFn encode;
-    int max_clusters[5];     // clusters of 1, 2, 4, 8, 16 blocks of the few-row kernel that fit the device at once
-    int small_clusters[kSmallCluster];   // clusters of 1, 2, .. blocks of the small fp32 kernel
-};
 
 #ifdef EVLN_TIMELINE
 // debug builds only (see timeline_debug.cuh): where the attention kernel leaves its clock stamps
@@ -51,26 +37,6 @@ extern "C" int evlnDebugSetTimeline(void* p)
 #endif
 
 namespace {
-
-// Every kernel is launched with programmatic stream serialisation: its prologue may overlap the
-// tail of the previous kernel in the stream; each kernel waits (griddepcontrol.wait) before it
-// touches global memory.
-template <typename... KArgs, typename... Args>
-cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
-                       Args&&... args)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
-}
 
 // The attention kernel runs as clusters of two CTAs (one CTA pair per work item).
 template <typename... KArgs, typename... Args>
@@ -171,56 +137,6 @@ bool attention_register_pool_ok()
         if (fa.numRegs != kRegsLaunch) return false;
     }
     return true;
-}
-
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-inline bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
-{
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return a_bytes > 0 && b_bytes > 0 && x < y + b_bytes && y < x + a_bytes;
-}
-inline int elem_bytes(int dtype) { return dtype == EVLN_BF16 ? 2 : 4; }
-
-evlnStatus_t cuda_fail(evlnHandle_t h, cudaError_t e)
-{
-    h->last_cuda_error = (int)e;
-    return EVLN_CUDA_ERROR;
-}
-
-// The handle's device must be current when work is launched: the kernels' attributes and the
-// tensor maps belong to that device's context.
-bool device_is_current(evlnHandle_t h)
-{
-    int dev = -1;
-    return cudaGetDevice(&dev) == cudaSuccess && dev == h->device;
-}
-
-// An optional position table must cover the positions [first, first + count) of the call.
-bool rope_table_covers(const void* table, int table_first, int table_count, long first, long count)
-{
-    if (!table) return true;
-    if (!aligned16(table) || table_first < 0 || table_count < 0) return false;
-    return (long)table_first <= first && first + count <= (long)table_first + table_count;
-}
-
-evlnStatus_t check_step_params(evlnHandle_t h, const evlnStepParams* p)
-{
-    if (!h || !p) return EVLN_INVALID_VALUE;
-    if (p->struct_size != sizeof(evlnStepParams)) return EVLN_INVALID_VALUE;
-    if (p->dtype != EVLN_BF16 && p->dtype != EVLN_F32) return EVLN_INVALID_VALUE;
-    if (p->num_q_heads <= 0 || p->num_kv_heads <= 0 || p->num_q_heads % p->num_kv_heads != 0)
-        return EVLN_INVALID_VALUE;
-    if (p->cache_len < 0 || p->num_new < 0 || p->cache_capacity < 0) return EVLN_INVALID_VALUE;
-    if (!(p->rope_theta > 0.0) || !(p->softmax_scale >= 0.f)) return EVLN_INVALID_VALUE;
-    if (p->num_splits < 0 || p->num_splits > kMaxSplits) return EVLN_INVALID_VALUE;
-    if (p->kernel != EVLN_KERNEL_AUTO && p->kernel != EVLN_KERNEL_SIMT) return EVLN_INVALID_VALUE;
-    if (p->head_dim != 64 && p->head_dim != 128) return EVLN_NOT_SUPPORTED;
-    if ((long)p->cache_len + p->num_new > (long)p->cache_capacity) return EVLN_CACHE_FULL;
-    if ((long)p->num_new * p->num_q_heads / p->num_kv_heads > (1 << 24)) return EVLN_NOT_SUPPORTED;
-    if (!rope_table_covers(p->rope_table, p->rope_table_first_pos, p->rope_table_count, p->cache_len, p->num_new))
-        return EVLN_INVALID_VALUE;
-    return EVLN_OK;
 }
 
 // fp32 on the tensor cores (attn_f32.cuh), unless the caller asks for the kernel without them, or for a softmax scale with which scores of
@@ -611,40 +527,6 @@ int resolve_splits(evlnHandle_t h, const evlnStepParams* p)
         return choose_splits_tc(units * p->num_kv_heads, (long)R * p->num_kv_heads, nkv_max, nkv_min, h->num_sms);
     }
     return simt_schedule(h, p, 0).splits;
-}
-
-bool encode_map(evlnHandle_t h, CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims,
-                const cuuint64_t* strides_bytes, const cuuint32_t* box)
-{
-    cuuint32_t ones[5] = {1, 1, 1, 1, 1};
-    CUresult r = h->encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base),
-                           dims, strides_bytes, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS;
-}
-
-evlnStatus_t check_paged_params(evlnHandle_t h, const evlnPagedParams* p, const int* lens, const int* offs)
-{
-    if (!h || !p || !lens || !offs) return EVLN_INVALID_VALUE;
-    if (p->struct_size != sizeof(evlnPagedParams)) return EVLN_INVALID_VALUE;
-    if (p->num_q_heads <= 0 || p->num_kv_heads <= 0 || p->num_q_heads % p->num_kv_heads != 0)
-        return EVLN_INVALID_VALUE;
-    if (p->batch < 1 || p->num_pages < 1 || p->max_pages_per_seq < 1 || p->kv_chunk_tiles < 0)
-        return EVLN_INVALID_VALUE;
-    if (!(p->rope_theta > 0.0) || !(p->softmax_scale >= 0.f)) return EVLN_INVALID_VALUE;
-    if (p->dtype != EVLN_BF16 || p->head_dim != 128 || p->page_size != 64 || p->batch > kMaxBatch)
-        return EVLN_NOT_SUPPORTED;
-    if (offs[0] != 0) return EVLN_INVALID_VALUE;
-    for (int b = 0; b < p->batch; ++b) {
-        if (lens[b] < 0 || offs[b + 1] < offs[b]) return EVLN_INVALID_VALUE;
-        const long tokens = (long)lens[b] + (offs[b + 1] - offs[b]);
-        if ((tokens + p->page_size - 1) / p->page_size > p->max_pages_per_seq) return EVLN_CACHE_FULL;
-        if (!rope_table_covers(p->rope_table, p->rope_table_first_pos, p->rope_table_count, lens[b], offs[b + 1] - offs[b]))
-            return EVLN_INVALID_VALUE;
-    }
-    if ((long)offs[p->batch] * p->num_q_heads / p->num_kv_heads > (1 << 24)) return EVLN_NOT_SUPPORTED;
-    return EVLN_OK;
 }
 
 // KV tiles of unit u of a batch item: paged episode, or item sharing a cache prefix (tail).
@@ -1135,6 +1017,7 @@ evlnStatus_t evlnCreate(evlnHandle_t* handle, int device)
     e = cudaMalloc(&h->d_status, sizeof(int));
     if (e == cudaSuccess) e = cudaMemset(h->d_status, 0, sizeof(int));
     if (e == cudaSuccess) e = prepare_kernels();
+    if (e == cudaSuccess) e = prepare_cache_kernels();
     if (e == cudaSuccess) e = query_few_clusters(h->max_clusters);
     if (e == cudaSuccess) e = query_small_clusters(h->small_clusters);
     if (e == cudaSuccess && !attention_register_pool_ok()) {
@@ -1964,20 +1847,6 @@ extern "C" evlnStatus_t evlnPackedForward(evlnHandle_t h, const evlnPackedParams
 }
 
 // ---- un-rotated store + frame sampler ------------------------------------------------------
-
-namespace {
-evlnStatus_t check_gather_params(evlnHandle_t h, const evlnGatherParams* p)
-{
-    if (!h || !p) return EVLN_INVALID_VALUE;
-    if (p->struct_size != sizeof(evlnGatherParams)) return EVLN_INVALID_VALUE;
-    if (p->dtype != EVLN_BF16 && p->dtype != EVLN_F32) return EVLN_INVALID_VALUE;
-    if (p->num_kv_heads <= 0 || p->store_capacity < 0 || p->work_capacity < 0) return EVLN_INVALID_VALUE;
-    if (!(p->rope_theta > 0.0)) return EVLN_INVALID_VALUE;
-    if (p->head_dim != 64 && p->head_dim != 128) return EVLN_NOT_SUPPORTED;
-    if (!device_is_current(h)) return EVLN_INVALID_VALUE;
-    return EVLN_OK;
-}
-}  // namespace
 
 extern "C" int evlnSampleFrames(int sampler, int num_frames, int budget, int stride, int* h_indices)
 {

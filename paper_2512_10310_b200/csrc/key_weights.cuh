@@ -1,0 +1,344 @@
+// The attention weight that a step's queries give each key:  w_j = sum_r 2^(s_rj - lse_r),  s = scale log2(e) q_r . k_j,
+// over the packed query rows r of a kv head that see key j, added to decay * (what the key had).
+//
+// Knowing each row's log-sum-exp, there is no running maximum and no order: the sum over rows wants the scores TRANSPOSED,
+// keys down and query rows across.  So a key is a lane of tensor memory (M = 128 keys a tile, N query rows), a thread owns a
+// key, and its sum is a loop over columns in its own registers: no shuffles and no atomics, and few rows cost few
+// columns instead of a padded 128-row tile.
+//
+// bf16: S^T = K Q^T on tcgen05 (kind::f16, fp32 sums).  Per CTA, 384 threads: warp 0 loads (TMA, a ring of K tiles and one of
+// query chunks), warp 1 issues, warps 4-11 exponentiate: two groups of four (one warp per TMEM lane quarter) that take the
+// chunks in turn, or whole tiles in turn where a tile is one chunk.  Score buffers: 4 x 128 columns.
+// Bound: many rows, the special-function unit (16 exponentials a cycle and SM; the products take a quarter of that); few
+// rows, reading the keys once.
+// Few tiles: the chunks of a tile are dealt to the CTAs of a cluster, whose sums meet in the first one's shared memory, in order.
+// fp32: a thread per key with its row in registers, query rows broadcast from shared memory, float FMAs.
+#pragma once
+
+#include <cuda.h>
+
+#include "common.cuh"
+#include "ptx_sm100.cuh"
+#include "tc_common.cuh"
+
+namespace evln {
+
+struct KeyWeightArgs {
+    const float* lse;        // [n, Hq]
+    const float* in;         // [Hkv, cap]
+    float* out;              // [Hkv, cap]
+    const void* q_rot;       // fp32 kernel: [Hkv, rows, D]
+    const void* k_cache;     // fp32 kernel: [Hkv, cap, D]
+    int* status;
+    int Hkv, G, rows, L, n, cap;
+    int chunk_rows, chunks;  // query rows of a chunk (the tensor kernel's N), chunks of a kv head
+    int items;               // kv heads * key tiles
+    float scale_log2, decay;
+    FastDiv div_g, div_hkv;
+};
+
+constexpr int kKwThreads = 384, kKwStages = 3, kKwBufs = 4, kKwMaxCluster = 8;
+template <int D>
+struct KeyWeightPlan {
+    static constexpr int kTile = 128 * D * 2;            // a K tile, a chunk of 128 query rows
+    static constexpr int kQOff = kKwStages * kTile, kBarOff = 2 * kKwStages * kTile;
+    static constexpr int kLseOff = kBarOff + 256;        // float [2 groups][2][128]
+    static constexpr int kPartOff = kLseOff + 2 * 2 * 128 * 4;       // float [2][128]: group 1's sums, tiles in turn
+    static constexpr int kRemoteOff = kPartOff + 2 * 128 * 4;        // float [kKwMaxCluster][128]
+    // (never two CTAs on an SM: each takes all of tensor memory, and CTAs of a cluster wait for each other)
+    static constexpr int kNeeded = kRemoteOff + kKwMaxCluster * 128 * 4 + 1024, kBytes = kNeeded < 120 * 1024 ? 120 * 1024 : kNeeded;
+    static_assert(kBytes <= 227 * 1024, "shared memory of a block");
+};
+
+// the first chunk of the tile at `key0` with a row that sees one of its keys
+__device__ __forceinline__ int first_chunk(const KeyWeightArgs& a, int key0)
+{
+    const int behind = key0 - a.L;                       // tokens before this one see none of the tile's keys
+    return behind <= 0 ? 0 : behind * a.G / a.chunk_rows;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kKwThreads, 1)
+key_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_q, const KeyWeightArgs a)
+{
+    using Plan = KeyWeightPlan<D>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
+    const uint32_t bar_k_full = smem_base + Plan::kBarOff, bar_k_empty = bar_k_full + 8 * kKwStages;
+    const uint32_t bar_q_full = bar_k_empty + 8 * kKwStages, bar_q_empty = bar_q_full + 8 * kKwStages;
+    const uint32_t bar_s_full = bar_q_empty + 8 * kKwStages, bar_s_free = bar_s_full + 8 * kKwBufs;
+    const uint32_t tmem_slot = bar_s_free + 8 * kKwBufs;
+    volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(smem_gen + (tmem_slot - smem_base));
+    volatile int* s_abort = reinterpret_cast<volatile int*>(smem_gen + (tmem_slot - smem_base) + 4);
+    float* s_lse = reinterpret_cast<float*>(smem_gen + Plan::kLseOff);
+    float* s_part = reinterpret_cast<float*>(smem_gen + Plan::kPartOff);
+    float* s_remote = reinterpret_cast<float*>(smem_gen + Plan::kRemoteOff);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // A CTA (cluster size 1) takes tiles blockIdx.x, + gridDim.x, ...; a cluster of several takes one, its chunks dealt out.
+    const int csize = (int)gridDim.y, rank = (int)blockIdx.y, stride = (int)gridDim.x;
+    auto tile_of = [&](int item, int& g) -> int {         // kv heads side by side
+        const int t = (int)fast_div((uint32_t)item, a.div_hkv);
+        g = item - t * a.Hkv;
+        return t * kTileN;
+    };
+
+    if (threadIdx.x == 0) {
+        ptx::prefetch_tensormap(&tm_k);
+        ptx::prefetch_tensormap(&tm_q);
+        for (int i = 0; i < kKwStages; ++i) {
+            ptx::mbar_init(bar_k_full + 8 * i, 1);
+            ptx::mbar_init(bar_k_empty + 8 * i, 1);
+            ptx::mbar_init(bar_q_full + 8 * i, 1);
+            ptx::mbar_init(bar_q_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < kKwBufs; ++i) {
+            ptx::mbar_init(bar_s_full + 8 * i, 1);
+            ptx::mbar_init(bar_s_free + 8 * i, 4);
+        }
+        ptx::fence_barrier_init();
+        *s_abort = 0;
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc(tmem_slot, 512);
+        ptx::tmem_relinquish();
+    }
+    ptx::fence_before_sync();
+    __syncthreads();
+    ptx::fence_after_sync();
+    const uint32_t tmem = *s_tmem;
+    if (csize > 1) ptx::cluster_arrive_relaxed();         // (waited for before the first remote store: all CTAs have started)
+    ptx::grid_launch_dependents();
+    ptx::grid_dependency_wait();
+
+    bool ok = true;
+    float own_sum = 0.f;                                  // cluster: this CTA's sums (group 0's threads)
+    if (warp == 0) {
+        if (lane == 0) {
+            int kt = 0, qt = 0;                           // tiles and chunks so far
+            for (int item = blockIdx.x; item < a.items && ok; item += stride, ++kt) {
+                int g;
+                const int key0 = tile_of(item, g), ks = kt % kKwStages;
+                bool fresh = true;
+                for (int c = first_chunk(a, key0) + rank; c < a.chunks && ok; c += csize, ++qt) {
+                    if (fresh) {
+                        if (kt >= kKwStages) ok = wait_bounded(bar_k_empty + 8 * ks, ((kt / kKwStages) & 1) ^ 1, kDevTimeoutProducer, a.status, s_abort);
+                        if (!ok) break;
+                        ptx::mbar_expect_tx(bar_k_full + 8 * ks, Plan::kTile);
+                        for (int d = 0; d < D; d += 64) ptx::tma_load_3d(smem_base + ks * Plan::kTile + d * 256, &tm_k, bar_k_full + 8 * ks, d, key0, g);
+                        fresh = false;
+                    }
+                    const int qs = qt % kKwStages;
+                    if (qt >= kKwStages) ok = wait_bounded(bar_q_empty + 8 * qs, ((qt / kKwStages) & 1) ^ 1, kDevTimeoutProducer, a.status, s_abort);
+                    if (!ok) break;
+                    ptx::mbar_expect_tx(bar_q_full + 8 * qs, a.chunk_rows * D * 2);
+                    for (int d = 0; d < D; d += 64)
+                        ptx::tma_load_3d(smem_base + Plan::kQOff + qs * Plan::kTile + d * 256, &tm_q, bar_q_full + 8 * qs, d, c * a.chunk_rows, g);
+                }
+                if (fresh) --kt;                          // no chunk of this CTA's: the tile was not loaded
+            }
+            if (!ok || *s_abort) {
+                const long long t0 = clock64();           // loads in flight land before the CTA may leave
+                while (clock64() - t0 < 400000) { }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        const uint32_t idesc = make_idesc(false, 128, a.chunk_rows);
+        const uint64_t kd0 = make_sdesc(smem_base, 16, 1024), qd0 = make_sdesc(smem_base + Plan::kQOff, 16, 1024);
+        int kt = 0, qt = 0;
+        for (int item = blockIdx.x; item < a.items && ok; item += stride) {
+            int g;
+            const int key0 = tile_of(item, g), ks = kt % kKwStages, c0 = first_chunk(a, key0) + rank;
+            for (int c = c0; c < a.chunks && ok; c += csize, ++qt) {
+                const int qs = qt % kKwStages, buf = qt % kKwBufs;
+                bool mine = true;
+                if (lane == 0 && c == c0) mine = wait_bounded(bar_k_full + 8 * ks, (kt / kKwStages) & 1, kDevTimeoutMmaKV, a.status, s_abort);
+                if (lane == 1) mine = wait_bounded(bar_q_full + 8 * qs, (qt / kKwStages) & 1, kDevTimeoutMmaQ, a.status, s_abort);
+                if (lane == 2 && qt >= kKwBufs) mine = wait_bounded(bar_s_free + 8 * buf, ((qt / kKwBufs) & 1) ^ 1, kDevTimeoutMmaP, a.status, s_abort);
+                ok = __all_sync(0xffffffffu, mine);
+                if (!ok) break;
+                ptx::fence_after_sync();
+                if (ptx::elect_one()) {
+                    const uint64_t kd = kd0 + (uint64_t)((ks * Plan::kTile) >> 4), qd = qd0 + (uint64_t)((qs * Plan::kTile) >> 4);
+#pragma unroll
+                    for (int s = 0; s < D / 16; ++s) {
+                        const uint64_t off = (uint64_t)(((s >> 2) * 64 * 256 + (s & 3) * 32) >> 4);
+                        ptx::mma_ss(tmem + buf * 128, kd + off, qd + off, idesc, s > 0);
+                    }
+                    ptx::mma_commit(bar_s_full + 8 * buf);
+                    ptx::mma_commit(bar_q_empty + 8 * qs);
+                    if (c + csize >= a.chunks) ptx::mma_commit(bar_k_empty + 8 * ks);
+                }
+                __syncwarp();
+            }
+            if (c0 < a.chunks) ++kt;
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp & 3, grp = (warp - 4) >> 2;
+        const int key_lane = (quarter << 5) + lane;       // = TMEM lane = the thread's key within a tile
+        const uint32_t t_lane = tmem + ((uint32_t)(quarter << 5) << 16);
+        float* my_lse = s_lse + grp * 256;
+        const bool turns = a.chunks == 1;                 // whole tiles in turn
+        const uint64_t scale2 = ptx::pack2(a.scale_log2, a.scale_log2);
+        int qt = 0, kt = 0, used = 0;                     // chunks, tiles; chunks of this group
+        auto meet = [&](int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); };
+        for (int item = blockIdx.x; item < a.items; item += stride) {
+            int g;
+            const int key0 = tile_of(item, g), key = key0 + key_lane, c0 = first_chunk(a, key0) + rank;
+            const bool writes = key < a.L + a.n && rank == 0 && (turns ? (kt & 1) == grp : grp == 0);
+            const float had = writes && key < a.L ? a.in[(long)g * a.cap + key] * a.decay : 0.f;
+            const int from = key > a.L ? (key - a.L) * a.G : 0;           // the first row that sees the key
+            const bool edge = key0 + kTileN - 1 > a.L;                    // (uniform) some key of the tile is not seen by all
+            uint64_t sum0 = 0, sum1 = 0;                                  // two floats each
+            for (int c = c0; c < a.chunks; c += csize, ++qt) {
+                if ((turns ? (kt & 1) : (qt & 1)) != grp) continue;
+                const int buf = qt % kKwBufs, row0 = c * a.chunk_rows, valid = min(a.chunk_rows, a.rows - row0);
+                float* lse = my_lse + (used & 1) * 128;
+                ++used;
+                float mine = INFINITY;                    // a row behind the last one counts as nothing
+                if (key_lane < valid) {
+                    const int r = row0 + key_lane, i = (int)fast_div((uint32_t)r, a.div_g);
+                    mine = a.lse[(long)i * (a.Hkv * a.G) + g * a.G + (r - i * a.G)] * 1.4426950408889634f;
+                }
+                lse[key_lane] = -mine;
+                meet(1 + grp, 128);                       // (the other buffer's readers are done: they met here since)
+                ok = ok && warp_wait(bar_s_full + 8 * buf, (qt / kKwBufs) & 1, kDevTimeoutSoftmaxS, a.status, s_abort, lane);
+                if (ok) {
+                    ptx::fence_after_sync();
+                    const bool plain = !edge && valid == a.chunk_rows;
+                    for (int col = 0; col < a.chunk_rows; col += 32) {
+                        uint32_t s[32];
+                        ptx::tmem_ld32(t_lane + buf * 128 + col, s);
+                        ptx::tmem_ld_wait();
+                        if (col + 32 >= a.chunk_rows) {
+                            ptx::fence_before_sync();
+                            if (ptx::elect_one()) ptx::mbar_arrive(bar_s_free + 8 * buf);
+                        }
+                        const float4* l4 = reinterpret_cast<const float4*>(lse + col);
+                        if (plain) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4) {
+                                const float4 m = l4[e >> 2];
+                                float x0, x1, x2, x3;
+                                ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), scale2, ptx::pack2(m.x, m.y)), x0, x1);
+                                ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), scale2, ptx::pack2(m.z, m.w)), x2, x3);
+                                sum0 = ptx::add2(sum0, ptx::pack2(ptx::ex2(x0), ptx::ex2(x1)));
+                                sum1 = ptx::add2(sum1, ptx::pack2(ptx::ex2(x2), ptx::ex2(x3)));
+                            }
+                        } else {
+                            const int lo = from - row0 - col, hi = valid - col;       // columns lo .. hi-1 count
+                            float add = 0.f;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                const float p = ptx::ex2(fmaf(__uint_as_float(s[e]), a.scale_log2, lse[col + e]));
+                                add += e >= lo && e < hi ? p : 0.f;
+                            }
+                            sum0 = ptx::add2(sum0, ptx::pack2(add, 0.f));
+                        }
+                    }
+                }
+            }
+            float u0, u1, u2, u3;
+            ptx::unpack2(sum0, u0, u1);
+            ptx::unpack2(sum1, u2, u3);
+            float sum = (u0 + u1) + (u2 + u3);
+            if (!turns) {
+                float* part = s_part + (kt & 1) * 128;
+                if (grp == 1) part[key_lane] = sum;
+                meet(3, 256);
+                if (grp == 0) sum += part[key_lane];
+            }
+            if (csize > 1) own_sum = sum;
+            else if (writes && ok) a.out[(long)g * a.cap + key] = had + sum;
+            ++kt;
+        }
+    }
+    if (csize > 1) {
+        // one tile per cluster: the sums of the other CTAs come to the first one's shared memory
+        const int key_lane = ((warp & 3) << 5) + lane;
+        __syncwarp();
+        ptx::cluster_wait();
+        if (warp >= 4 && warp < 8 && rank > 0) {
+            const uint32_t to = ptx::map_to_cta(smem_base + Plan::kRemoteOff + (rank * 128 + key_lane) * 4, 0);
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(own_sum) : "memory");
+        }
+        __syncwarp();
+        ptx::cluster_arrive();
+        ptx::cluster_wait();
+        if (warp >= 4 && warp < 8 && rank == 0) {
+            int g;
+            const int key = tile_of(blockIdx.x, g) + key_lane;
+            float sum = own_sum;
+            for (int r = 1; r < csize; ++r) sum += s_remote[r * 128 + key_lane];
+            if (key < a.L + a.n && ok) a.out[(long)g * a.cap + key] = (key < a.L ? a.in[(long)g * a.cap + key] * a.decay : 0.f) + sum;
+        }
+    }
+    ptx::fence_before_sync();
+    __syncthreads();
+    if (warp == 1) ptx::tmem_dealloc(tmem, 512);
+}
+
+// ---- fp32: a thread per key -------------------------------------------------------------------
+constexpr int kKwF32Keys = 128, kKwF32Rows = 16;          // keys of a block, query rows staged at a time
+template <int D>
+__global__ void __launch_bounds__(kKwF32Keys)
+key_weights_f32_kernel(const KeyWeightArgs a)
+{
+    __shared__ __align__(16) float s_q[kKwF32Rows][D];
+    __shared__ float s_lse[kKwF32Rows];
+    __shared__ float s_remote[kKwMaxCluster][kKwF32Keys];
+    const int csize = (int)gridDim.y, rank = (int)blockIdx.y;
+    const int t = (int)fast_div(blockIdx.x, a.div_hkv), g = (int)blockIdx.x - t * a.Hkv;
+    const int key0 = t * kKwF32Keys, key = key0 + (int)threadIdx.x, total = a.L + a.n;
+    if (csize > 1) ptx::cluster_arrive_relaxed();
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
+    float k[D];
+    {
+        const float4* row = reinterpret_cast<const float4*>((const float*)a.k_cache + ((long)g * a.cap + min(key, total - 1)) * D);
+#pragma unroll
+        for (int d = 0; d < D; d += 4) {
+            const float4 v = row[d >> 2];
+            k[d] = v.x; k[d + 1] = v.y; k[d + 2] = v.z; k[d + 3] = v.w;
+        }
+    }
+    const int from = key > a.L ? (key - a.L) * a.G : 0;   // the first row that sees the key
+    float sum = 0.f;
+    for (int c = first_chunk(a, key0) + rank; c < a.chunks; c += csize) {
+        const int row0 = c * kKwF32Rows, valid = min(kKwF32Rows, a.rows - row0);
+        __syncthreads();
+        const float4* src = reinterpret_cast<const float4*>((const float*)a.q_rot + ((long)g * a.rows + row0) * D);
+        for (int e = threadIdx.x; e < valid * D / 4; e += kKwF32Keys) reinterpret_cast<float4*>(&s_q[0][0])[e] = src[e];
+        if ((int)threadIdx.x < valid) {
+            const int r = row0 + (int)threadIdx.x, i = (int)fast_div((uint32_t)r, a.div_g);
+            s_lse[threadIdx.x] = a.lse[(long)i * (a.Hkv * a.G) + g * a.G + (r - i * a.G)] * 1.4426950408889634f;
+        }
+        __syncthreads();
+        for (int r = 0; r < valid; ++r) {
+            float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+            for (int d = 0; d < D; d += 4) {
+                const float4 q = *reinterpret_cast<const float4*>(&s_q[r][d]);
+                s0 = fmaf(q.x, k[d], s0); s1 = fmaf(q.y, k[d + 1], s1); s2 = fmaf(q.z, k[d + 2], s2); s3 = fmaf(q.w, k[d + 3], s3);
+            }
+            const float p = exp2f(fmaf((s0 + s1) + (s2 + s3), a.scale_log2, -s_lse[r]));
+            sum += row0 + r >= from ? p : 0.f;
+        }
+    }
+    if (csize > 1) {
+        ptx::cluster_wait();
+        if (rank > 0) {
+            const uint32_t to = ptx::map_to_cta(ptx::smem_u32(&s_remote[rank][threadIdx.x]), 0);
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(sum) : "memory");
+        }
+        ptx::cluster_arrive();
+        ptx::cluster_wait();
+        if (rank > 0) return;
+        for (int r = 1; r < csize; ++r) sum += s_remote[r][threadIdx.x];
+    }
+    if (key < total) a.out[(long)g * a.cap + key] = (key < a.L ? a.in[(long)g * a.cap + key] * a.decay : 0.f) + sum;
+}
+
+}  // namespace evln

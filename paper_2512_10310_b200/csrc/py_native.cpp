@@ -23,6 +23,7 @@ PyTypeObject* g_step_type = nullptr;
 PyTypeObject* g_paged_type = nullptr;
 PyTypeObject* g_packed_type = nullptr;
 PyTypeObject* g_gather_type = nullptr;
+PyTypeObject* g_norm_type = nullptr;
 PyObject* g_error = nullptr;             // EvlnError(status, where)
 PyObject* g_argument_error = nullptr;    // a parameter structure of the wrong type
 
@@ -522,16 +523,187 @@ EVLN_ENTRY(py_gather_rope)
     });
 }
 
-// configure(step_type, paged_type, packed_type, gather_type, EvlnError, ArgumentError)
+// an evlnHeadNorm, or None: a null pointer in *use
+bool as_norm(PyObject* o, evlnHeadNorm* n, const evlnHeadNorm** use)
+{
+    *use = nullptr;
+    if (is_none(o)) return true;
+    *use = n;
+    return as_params(o, g_norm_type, n);
+}
+
+EVLN_ENTRY(py_norm_rope_append)
+{
+    static const char* const names[] = {"handle", "params", "norm", "q_new", "k_new", "v_new", "q_rot", "k_cache", "v_cache", "stream", "strides", nullptr};
+    PyObject* a[kMaxArgs];
+    if (!take_args("evlnNormRopeAppend", args, nargs, kwnames, names, 9, a)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        evlnHandle_t h;
+        evlnStepParams p;
+        evlnHeadNorm norm;
+        const evlnHeadNorm* use;
+        void* t[6];
+        void* st;
+        long s[3];
+        if (!token_strides(a[10], a[3], a[4], a[5], s) || !as_handle(a[0], &h) || !as_params(a[1], g_step_type, &p) || !as_norm(a[2], &norm, &use)) return nullptr;
+        for (int i = 0; i < 6; ++i)
+            if (!as_pointer(a[3 + i], &t[i])) return nullptr;
+        if (!as_stream(a[9], &st)) return nullptr;
+        return finish(unlocked([&] { return evlnNormRopeAppend(h, &p, use, t[0], t[1], t[2], s[0], s[1], s[2], t[3], t[4], t[5], st); }), "evlnNormRopeAppend");
+    });
+}
+
+EVLN_ENTRY(py_paged_norm_rope_append)
+{
+    static const char* const names[] = {"handle", "params", "norm", "q_new", "k_new", "v_new", "cache_lens", "new_offsets", "page_table", "q_rot", "k_pool",
+                                        "v_pool", "stream", "strides", nullptr};
+    PyObject* a[kMaxArgs];
+    if (!take_args("evlnPagedNormRopeAppend", args, nargs, kwnames, names, 12, a)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        evlnHandle_t h;
+        evlnPagedParams p;
+        evlnHeadNorm norm;
+        const evlnHeadNorm* use;
+        std::vector<int> lens, offs;
+        void *t[3], *to[4], *st;
+        long s[3];
+        if (!token_strides(a[13], a[3], a[4], a[5], s) || !as_handle(a[0], &h) || !as_params(a[1], g_paged_type, &p) || !as_norm(a[2], &norm, &use) ||
+            !paged_arrays(p, a[6], a[7], &lens, &offs))
+            return nullptr;
+        for (int i = 0; i < 3; ++i)
+            if (!as_pointer(a[3 + i], &t[i])) return nullptr;
+        for (int i = 0; i < 4; ++i)
+            if (!as_pointer(a[8 + i], &to[i])) return nullptr;
+        if (!as_stream(a[12], &st)) return nullptr;
+        return finish(unlocked([&] {
+            return evlnPagedNormRopeAppend(h, &p, use, t[0], t[1], t[2], s[0], s[1], s[2], lens.data(), offs.data(), (const int*)to[0], to[1], to[2], to[3], st);
+        }), "evlnPagedNormRopeAppend");
+    });
+}
+
+EVLN_ENTRY(py_paged8_rope_append)
+{
+    static const char* const names[] = {"handle", "params", "norm", "q_new", "k_new", "v_new", "cache_lens", "new_offsets", "page_table", "q_rot", "k_pool",
+                                        "v_pool", "k_scale", "v_scale", "stream", "strides", nullptr};
+    PyObject* a[kMaxArgs];
+    if (!take_args("evlnPaged8RopeAppend", args, nargs, kwnames, names, 14, a)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        evlnHandle_t h;
+        evlnPagedParams p;
+        evlnHeadNorm norm;
+        const evlnHeadNorm* use;
+        std::vector<int> lens, offs;
+        void *t[3], *to[6], *st;
+        long s[3];
+        if (!token_strides(a[15], a[3], a[4], a[5], s) || !as_handle(a[0], &h) || !as_params(a[1], g_paged_type, &p) || !as_norm(a[2], &norm, &use) ||
+            !paged_arrays(p, a[6], a[7], &lens, &offs))
+            return nullptr;
+        for (int i = 0; i < 3; ++i)
+            if (!as_pointer(a[3 + i], &t[i])) return nullptr;
+        for (int i = 0; i < 6; ++i)
+            if (!as_pointer(a[8 + i], &to[i])) return nullptr;
+        if (!as_stream(a[14], &st)) return nullptr;
+        return finish(unlocked([&] {
+            return evlnPaged8RopeAppend(h, &p, use, t[0], t[1], t[2], s[0], s[1], s[2], lens.data(), offs.data(), (const int*)to[0], to[1], to[2], to[3],
+                                        (float*)to[4], (float*)to[5], st);
+        }), "evlnPaged8RopeAppend");
+    });
+}
+
+EVLN_ENTRY(py_paged8_step_attention)
+{
+    static const char* const names[] = {"handle", "params", "q_rot", "k_pool", "v_pool", "k_scale", "v_scale", "cache_lens", "new_offsets", "page_table",
+                                        "workspace", "out", "lse_out", "workspace_bytes", "stream", nullptr};
+    PyObject* a[kMaxArgs];
+    if (!take_args("evlnPaged8StepAttention", args, nargs, kwnames, names, 12, a)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        evlnHandle_t h;
+        evlnPagedParams p;
+        std::vector<int> lens, offs;
+        void *t[5], *u[4], *st;
+        size_t bytes;
+        if (!buffer_bytes(a[13], a[10], &bytes) || !as_handle(a[0], &h) || !as_params(a[1], g_paged_type, &p) || !paged_arrays(p, a[7], a[8], &lens, &offs))
+            return nullptr;
+        for (int i = 0; i < 5; ++i)
+            if (!as_pointer(a[2 + i], &t[i])) return nullptr;
+        for (int i = 0; i < 4; ++i)
+            if (!as_pointer(a[9 + i], &u[i])) return nullptr;
+        if (!as_stream(a[14], &st)) return nullptr;
+        return finish(unlocked([&] {
+            return evlnPaged8StepAttention(h, &p, t[0], t[1], t[2], (const float*)t[3], (const float*)t[4], lens.data(), offs.data(), (const int*)u[0], u[1],
+                                           bytes, u[2], (float*)u[3], st);
+        }), "evlnPaged8StepAttention");
+    });
+}
+
+EVLN_ENTRY(py_key_weights)
+{
+    static const char* const names[] = {"handle", "params", "q_rot", "k_cache", "lse", "decay", "weights_in", "weights_out", "stream", nullptr};
+    PyObject* a[kMaxArgs];
+    if (!take_args("evlnKeyWeights", args, nargs, kwnames, names, 8, a)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        evlnHandle_t h;
+        evlnStepParams p;
+        void *q, *k, *lse, *in, *out, *st;
+        if (!as_handle(a[0], &h) || !as_params(a[1], g_step_type, &p) || !as_pointer(a[2], &q) || !as_pointer(a[3], &k) || !as_pointer(a[4], &lse)) return nullptr;
+        const double decay = PyFloat_AsDouble(a[5]);
+        if (decay == -1.0 && PyErr_Occurred()) return nullptr;
+        if (!as_pointer(a[6], &in) || !as_pointer(a[7], &out) || !as_stream(a[8], &st)) return nullptr;
+        return finish(unlocked([&] { return evlnKeyWeights(h, &p, q, k, (const float*)lse, (float)decay, (const float*)in, (float*)out, st); }), "evlnKeyWeights");
+    });
+}
+
+EVLN_ENTRY(py_select_keys)
+{
+    static const char* const names[] = {"handle", "params", "weights", "num_keys", "budget", "sinks", "recent", "kept", "stream", nullptr};
+    PyObject* a[kMaxArgs];
+    if (!take_args("evlnSelectKeys", args, nargs, kwnames, names, 8, a)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        evlnHandle_t h;
+        evlnGatherParams p;
+        void *w, *kept, *st;
+        int v[4];
+        if (!as_handle(a[0], &h) || !as_params(a[1], g_gather_type, &p) || !as_pointer(a[2], &w)) return nullptr;
+        for (int i = 0; i < 4; ++i)
+            if (!as_int(a[3 + i], &v[i])) return nullptr;
+        if (!as_pointer(a[7], &kept) || !as_stream(a[8], &st)) return nullptr;
+        return finish(unlocked([&] { return evlnSelectKeys(h, &p, (const float*)w, v[0], v[1], v[2], v[3], (int*)kept, st); }), "evlnSelectKeys");
+    });
+}
+
+EVLN_ENTRY(py_gather_keys)
+{
+    static const char* const names[] = {"handle", "params", "num_kept", "kept", "weights", "k_store", "v_store", "weights_work", "k_work", "v_work", "rotate",
+                                        "stream", nullptr};
+    PyObject* a[kMaxArgs];
+    if (!take_args("evlnGatherKeys", args, nargs, kwnames, names, 10, a)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        evlnHandle_t h;
+        evlnGatherParams p;
+        void *t[7], *st;
+        int n;
+        if (!as_handle(a[0], &h) || !as_params(a[1], g_gather_type, &p) || !as_int(a[2], &n)) return nullptr;
+        for (int i = 0; i < 7; ++i)
+            if (!as_pointer(a[3 + i], &t[i])) return nullptr;
+        const int rotate = a[10] ? PyObject_IsTrue(a[10]) : 1;
+        if (rotate < 0 || !as_stream(a[11], &st)) return nullptr;
+        return finish(unlocked([&] {
+            return evlnGatherKeys(h, &p, n, (const int*)t[0], (const float*)t[1], t[2], t[3], (float*)t[4], t[5], t[6], rotate, st);
+        }), "evlnGatherKeys");
+    });
+}
+
+// configure(step_type, paged_type, packed_type, gather_type, norm_type, EvlnError, ArgumentError)
 PyObject* py_configure(PyObject*, PyObject* args)
 {
-    PyObject *s, *g, *k, *q, *e, *ae;
-    if (!PyArg_ParseTuple(args, "O!O!O!O!OO", &PyType_Type, &s, &PyType_Type, &g, &PyType_Type, &k, &PyType_Type, &q, &e, &ae)) return nullptr;
-    for (PyObject* o : {s, g, k, q, e, ae}) Py_INCREF(o);      // kept for the life of the process
+    PyObject *s, *g, *k, *q, *n, *e, *ae;
+    if (!PyArg_ParseTuple(args, "O!O!O!O!O!OO", &PyType_Type, &s, &PyType_Type, &g, &PyType_Type, &k, &PyType_Type, &q, &PyType_Type, &n, &e, &ae)) return nullptr;
+    for (PyObject* o : {s, g, k, q, n, e, ae}) Py_INCREF(o);      // kept for the life of the process
     g_step_type = (PyTypeObject*)s;
     g_paged_type = (PyTypeObject*)g;
     g_packed_type = (PyTypeObject*)k;
     g_gather_type = (PyTypeObject*)q;
+    g_norm_type = (PyTypeObject*)n;
     g_error = e;
     g_argument_error = ae;
     Py_RETURN_NONE;
@@ -555,6 +727,13 @@ PyMethodDef kMethods[] = {
                 "library (at most EVLN_NOALLOC_SCRATCH_BYTES); calls sharing a device must not overlap."),
     EVLN_METHOD("evlnStoreAppend", py_store_append, "The new frame's un-rotated keys and values to the store."),
     EVLN_METHOD("evlnGatherRope", py_gather_rope, "Lays the kept store segments out in the working cache; returns the number of tokens laid out."),
+    EVLN_METHOD("evlnNormRopeAppend", py_norm_rope_append, "evlnRopeAppend with a norm of every query and key head in the same pass (norm: head_norm(...))."),
+    EVLN_METHOD("evlnPagedNormRopeAppend", py_paged_norm_rope_append, "evlnPagedRopeAppend with a norm of every query and key head in the same pass."),
+    EVLN_METHOD("evlnPaged8RopeAppend", py_paged8_rope_append, "evlnPagedRopeAppend (norm None) or evlnPagedNormRopeAppend into a cache of 8-bit codes."),
+    EVLN_METHOD("evlnPaged8StepAttention", py_paged8_step_attention, "Step attention over a paged cache of 8-bit codes, into `out`."),
+    EVLN_METHOD("evlnKeyWeights", py_key_weights, "The attention weight that a step gave each key, added to decay * weights_in."),
+    EVLN_METHOD("evlnSelectKeys", py_select_keys, "The slots of each kv head to keep: first, last and of largest weight."),
+    EVLN_METHOD("evlnGatherKeys", py_gather_keys, "Lays the chosen slots of each kv head out back to back, keys turned at their new positions or copied."),
     {nullptr, nullptr, 0, nullptr},
 };
 
