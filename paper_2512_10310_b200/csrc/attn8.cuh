@@ -12,13 +12,16 @@
 //    2^-11, finer than bf16.)
 // The operands come out of ldmatrix as bytes: a key's 16 bytes are a k-step of the score product (four channels a lane, the
 // queries are laid out the same way), and a transposed load of byte PAIRS gives two keys of two neighbouring channels,
-// which one byte permutation parts into the operands of two column tiles.
+// which one byte permutation parts.  The second product is transposed, O^T = V^T P^T: what the scores leave in a lane's registers is
+// its right operand as it stands, and 8 rows (a token of 8 query heads a kv head) are one column tile, not half of a row tile.
 //
-// A block: 8 warps, RG row groups x KG key groups, each warp 16 MT rows.  A key group has a ring of its own of 32-key stages
-// (4 KB keys + 4 KB values, TMA, 128-byte swizzle), which one warp of it refills itself as it goes: warps of different key
-// groups never wait for each other before the block's merge.  The lanes of a warp look 32 stages ahead for page numbers and
-// scales (a lane each).  A block per SM, each with an equal share of the batch's stages, walked unit by unit (unit: episode, kv
-// head, tile of rows); a unit that the shares cut leaves normalised parts, which merge8_kernel joins.
+// A block: RG row groups x KG key groups of warps, each warp 8 NQ rows.  A key group takes a RUN of neighbouring stages (32 keys:
+// 4 KB keys + 4 KB values, TMA, 128-byte swizzle) through a ring of its own, which one warp of it refills as it goes, and walks it
+// unit by unit (unit: episode, kv head, tile of rows).  Nothing is shared between key groups until all are done: then the
+// results of neighbouring runs that ended in the same unit are joined in the shared memory that the rings leave.  (Stages dealt
+// to the warps in turn, which joins all of them at the end of every unit, took 45 us for 16 ragged episodes of a token, runs 38.)
+// Runs are equally long, KG of them per SM; a unit that the runs cut across blocks leaves normalised parts, which merge8_kernel
+// joins.  The lanes of a warp look 32 stages ahead for page numbers and scales (a lane each).
 // A row's reference m follows its maximum only when that is 2^8 above it, so outputs are rarely scaled anew.
 #pragma once
 
@@ -31,27 +34,32 @@
 
 namespace evln {
 
-constexpr int kA8Keys = 32, kA8StageBytes = 2 * kA8Keys * 128, kA8Warps = 8, kA8Threads = 32 * kA8Warps;
-constexpr int kA8QStride = 288;                       // bytes between query rows in shared memory (256 + a bank spread)
-constexpr int kA8OStride = 132;                       // floats between rows of the merge buffers
+constexpr int kA8Keys = 32, kA8StageBytes = 2 * kA8Keys * 128;
+constexpr int kA8OStride = 136;                       // floats between rows of the joint's buffers (neighbouring rows start 8 banks apart)
 constexpr float kA8Headroom = 8.f, kA8Lift = 6.f;     // p' <= 2^(headroom + lift), below the largest half
 constexpr float kA8LeastRatio = -40.f;                // log2 of the smallest value-scale ratio that is told apart (halves end at -24 - lift)
 
-template <int MT, int RG>
+template <int NQ, int RG>
 struct Attn8Plan {
-    static constexpr int kRows = 16 * MT * RG;
-    static constexpr int kKeyGroups = kA8Warps / RG;
-    static constexpr int kBufs = 2;
-    static constexpr int kQBytes = kRows * kA8QStride, kMergeBytes = kBufs * kRows * kA8OStride * 4;
-    static constexpr int kStatBytes = kKeyGroups * kRows * 8 + kRows * 4;
+    // up to 16 rows: twelve warps of 168 registers (three a scheduler hide each other's chains); 32: eight of 255
+    static constexpr int kWarps = NQ <= 2 ? 12 : 8, kThreads = 32 * kWarps;
+    // (8 rows need no more than 144, which leaves the SM room for blocks of the merge kernel)
+    static constexpr int kRegs = NQ == 1 ? 144 : NQ == 2 ? 168 : 255;
+    static constexpr int kWarpRows = 8 * NQ, kRows = kWarpRows * RG;
+    static constexpr int kKeyGroups = kWarps / RG;
+    static constexpr bool kQRegs = NQ <= 2;                                     // queries in registers, or in shared memory in operand order
+    static constexpr int kQBytes = kQRegs ? 0 : kWarps * (NQ / 2) * 8 * 512;
+    static constexpr int kStatBytes = kWarps * kWarpRows * 8 + 64;             // references and sums, the units that the runs ended in
     static constexpr int kBarBytes = 512;
-    static constexpr int kRest = kQBytes + kMergeBytes + kStatBytes + kBarBytes + 1024;
-    static constexpr int kSlots = (227 * 1024 - kRest) / kA8StageBytes / kKeyGroups < 32 ? (227 * 1024 - kRest) / kA8StageBytes / kKeyGroups : 32;
+    static constexpr int kRest = kQBytes + kStatBytes + kBarBytes + 1024;
+    static constexpr int kFit = (227 * 1024 - kRest) / kA8StageBytes / kKeyGroups;
+    static constexpr int kSlots = kFit < 32 ? kFit : 32;
     static constexpr int kRing = kKeyGroups * kSlots * kA8StageBytes;
-    static constexpr int kQOff = kRing, kMergeOff = kQOff + kQBytes, kStatOff = kMergeOff + kMergeBytes, kBarOff = kStatOff + kStatBytes;
+    static constexpr int kQOff = kRing, kStatOff = kQOff + kQBytes, kBarOff = kStatOff + kStatBytes;
     static constexpr int kBytes = kRing + kRest;
     static_assert(kSlots >= 2, "a stage in flight beside the one that is read");
     static_assert(16 * kKeyGroups * kSlots + 8 <= kBarBytes, "barriers");
+    static_assert(kWarps * kWarpRows * kA8OStride * 4 <= kRing + kQBytes, "the joint's buffers");
     static_assert(kBarOff % 8 == 0 && kBytes <= 227 * 1024, "shared memory of a block");
 };
 
@@ -62,11 +70,11 @@ struct Attn8Args {
     const int* page_table;
     __nv_bfloat16* out;              // [tokens, Hq, 128]
     float* lse_out;                  // [tokens, Hq] or null
-    float* o_part;                   // [2 * blocks, rows of a tile, 128]
-    float* lse_part;                 // [2 * blocks, rows of a tile], log2
+    float* o_part;                   // [2 * runs, rows of a tile, 128]
+    float* lse_part;                 // [2 * runs, rows of a tile], log2
     int* status;
     int Hkv, G, rows, batch, max_pages;
-    int share, total;                // stages of a block, of the batch
+    int run, total;                  // stages of a run, of the batch
     float scale_log2;
     FastDiv div_g;
 };
@@ -109,19 +117,27 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
     return r;
 }
 
-template <int MT, int RG>
-__global__ void __launch_bounds__(kA8Threads, 1)
+// Where query row rl of a unit goes: row of [tokens, Hq].
+__device__ __forceinline__ long out_row8(const Attn8Args& a, const BatchLens& lens, const Unit8& u, int rl)
+{
+    const int tok = (int)fast_div((uint32_t)rl, a.div_g);
+    return ((long)lens.new_off[u.b] + tok) * (a.Hkv * a.G) + u.g * a.G + (rl - tok * a.G);
+}
+constexpr float kLn2 = 0.69314718055994531f;
+
+template <int NQ, int RG>
+__global__ void __launch_bounds__(Attn8Plan<NQ, RG>::kThreads) __maxnreg__((Attn8Plan<NQ, RG>::kRegs))
 attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Attn8Args a, const __grid_constant__ BatchLens lens)
 {
-    using Plan = Attn8Plan<MT, RG>;
-    constexpr int ROWS = Plan::kRows, KG = Plan::kKeyGroups, SLOTS = Plan::kSlots;
+    using Plan = Attn8Plan<NQ, RG>;
+    constexpr int ROWS = Plan::kRows, KG = Plan::kKeyGroups, SLOTS = Plan::kSlots, WROWS = Plan::kWarpRows;
+    constexpr int MT = (NQ + 1) / 2, HN = NQ == 1 ? 1 : 2;              // 16-row tiles of the score products, 8-row halves of them in use
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
-    float* s_o = reinterpret_cast<float*>(smem_gen + Plan::kMergeOff);             // [kBufs][ROWS][kA8OStride]
-    float* s_m = reinterpret_cast<float*>(smem_gen + Plan::kStatOff);              // [KG][ROWS]
-    float* s_l = s_m + KG * ROWS;                                                  // [KG][ROWS]
-    float* s_c = s_l + KG * ROWS;                                                  // [ROWS] score factor of a row
+    float* s_m = reinterpret_cast<float*>(smem_gen + Plan::kStatOff);              // [warp][WROWS]
+    float* s_l = s_m + Plan::kWarps * WROWS;
+    int* s_unit = reinterpret_cast<int*>(s_l + Plan::kWarps * WROWS);              // [KG] first stage of the unit that the run ended in, -1: nothing left
     volatile int* s_abort = reinterpret_cast<volatile int*>(smem_gen + Plan::kBarOff + 16 * KG * SLOTS);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = lane & 3, lrow = lane >> 2;
@@ -129,120 +145,154 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     const uint32_t ring = smem_base + kg * SLOTS * kA8StageBytes;
     const uint32_t bar_full = smem_base + Plan::kBarOff + 16 * kg * SLOTS, bar_empty = bar_full + 8 * SLOTS;
 
-    const int s0 = blockIdx.x * a.share, s1 = min(a.total, s0 + a.share);          // the block's stages
-    const int mine = s1 - s0 > kg ? (s1 - s0 - kg + KG - 1) / KG : 0;              // of them this key group's: s0 + kg + i KG
+    const int run = blockIdx.x * KG + kg;
+    const int r0 = min(a.total, run * a.run), r1 = min(a.total, r0 + a.run), mine = r1 - r0;      // the run: stages r0 .. r1-1
 
-    if (tid == 0) {
-        *s_abort = 0;
-        for (int k = 0; k < KG; ++k)
-            for (int i = 0; i < SLOTS; ++i) {
-                ptx::mbar_init(smem_base + Plan::kBarOff + 16 * k * SLOTS + 8 * i, 1);
-                ptx::mbar_init(smem_base + Plan::kBarOff + 16 * k * SLOTS + 8 * (SLOTS + i), RG);
-            }
+    if (lane == 0 && rg == 0) {
+        for (int i = 0; i < SLOTS; ++i) {
+            ptx::mbar_init(bar_full + 8 * i, 1);
+            ptx::mbar_init(bar_empty + 8 * i, RG);
+        }
         ptx::fence_barrier_init();
-        ptx::prefetch_tensormap(&tm_k);
-        ptx::prefetch_tensormap(&tm_v);
+        if (warp == 0) {
+            *s_abort = 0;
+            ptx::prefetch_tensormap(&tm_k);
+            ptx::prefetch_tensormap(&tm_v);
+        }
     }
+    Unit8 u = {};
+    if (mine > 0) u = unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, r0);
     __syncthreads();
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
 
-    // ---- looking ahead: lane j knows stage 32 w + j of the key group for window w ----
+    // ---- looking ahead: lane j knows stage 32 w + j of the run for window w ----
     struct Ahead { int row; float ks, vs; };           // first row of the code pools, scales
     auto look = [&](int window) -> Ahead {
         const int i = 32 * window + lane;
         Ahead h = {0, 0.f, 0.f};
         if (i < mine) {
-            const int s = s0 + kg + i * KG;
-            const Unit8 u = unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, s);
-            const int key = (s - u.first) * kA8Keys;
-            const int page = a.page_table[(long)u.b * a.max_pages + key / kPage8], at = page * a.Hkv + u.g;
+            Unit8 w = u;
+            if (r0 + i >= u.first + u.stages) w = unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, r0 + i);
+            const int key = (r0 + i - w.first) * kA8Keys;
+            const int page = a.page_table[(long)w.b * a.max_pages + key / kPage8], at = page * a.Hkv + w.g;
             h.row = at * kPage8 + (key & (kPage8 - 1));
             h.ks = a.k_scale[at];
             h.vs = a.v_scale[at];
         }
         return h;
     };
-    auto load = [&](int i, int row) {                  // one lane
-        const uint32_t dst = ring + (i % SLOTS) * kA8StageBytes, bar = bar_full + 8 * (i % SLOTS);
+    auto load = [&](int slot, int row) {               // one lane
+        const uint32_t dst = ring + slot * kA8StageBytes, bar = bar_full + 8 * slot;
         ptx::mbar_expect_tx(bar, kA8StageBytes);
         ptx::tma_load_2d(dst, &tm_k, bar, 0, row);
         ptx::tma_load_2d(dst + kA8StageBytes / 2, &tm_v, bar, 0, row);
     };
-    Ahead now = look(0), next = look(1);
-    if (rg == 0 && lane < SLOTS && lane < mine) load(lane, now.row);
-    __syncwarp();
+    // ---- a unit's queries: halves of each row's own size, in operand order (k-step c: channels 16 c + 4 quad .. + 3 of rows lrow, lrow + 8) ----
+    uint4* q_at = reinterpret_cast<uint4*>(smem_gen + Plan::kQOff + warp * (MT * 8 * 512)) + lane;
+    uint32_t qf[Plan::kQRegs ? 8 : 1][2 * HN];
+    float factor[MT][HN];
+    auto load_q = [&](int mt, uint2 (&raw)[HN][8]) {
+#pragma unroll
+        for (int h = 0; h < HN; ++h) {
+            const int rl = u.tile * ROWS + rg * WROWS + mt * 16 + h * 8 + lrow;
+            const uint2* src = reinterpret_cast<const uint2*>(a.q_rot + ((long)u.g * a.rows + (long)lens.new_off[u.b] * a.G + rl) * 128) + quad;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) raw[h][c] = rl < u.n * a.G ? src[4 * c] : make_uint2(0u, 0u);
+        }
+    };
+    auto put_q = [&](int mt, const uint2 (&raw)[HN][8]) {
+        float up[HN];
+#pragma unroll
+        for (int h = 0; h < HN; ++h) {
+            float most = 0.f;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                most = ptx::max3(most, fabsf(__uint_as_float(raw[h][c].x << 16)), fabsf(__uint_as_float(raw[h][c].x & 0xffff0000u)));
+                most = ptx::max3(most, fabsf(__uint_as_float(raw[h][c].y << 16)), fabsf(__uint_as_float(raw[h][c].y & 0xffff0000u)));
+            }
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            int e = 14 - ((int)(__float_as_uint(most) >> 23) - 127);                 // the row's maximum into [2^14, 2^15)
+            e = e > 100 ? 100 : e;
+            up[h] = exp2_int(e);
+            factor[mt][h] = a.scale_log2 * exp2_int(-e);
+        }
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            uint32_t f[2 * HN];                                                       // channels 4 quad, + 1 of each half, then + 2, + 3
+#pragma unroll
+            for (int h = 0; h < HN; ++h) {
+                f[h] = pack_f16x2(__uint_as_float(raw[h][c].x << 16) * up[h], __uint_as_float(raw[h][c].x & 0xffff0000u) * up[h]);
+                f[h + HN] = pack_f16x2(__uint_as_float(raw[h][c].y << 16) * up[h], __uint_as_float(raw[h][c].y & 0xffff0000u) * up[h]);
+            }
+            if constexpr (Plan::kQRegs) {
+#pragma unroll
+                for (int e = 0; e < 2 * HN; ++e) qf[c][e] = f[e];
+            } else {
+                q_at[(mt * 8 + c) * 32] = make_uint4(f[0], f[1], f[2], f[3]);         // (read by this lane only)
+            }
+        }
+    };
+
+    Ahead now, next;
+    {
+        // the first unit's queries are on their way while the first stages' pages are looked up
+        uint2 raw[HN][8];
+        if (mine > 0) load_q(0, raw);
+        now = look(0);
+        if (rg == 0 && lane < SLOTS && lane < mine) load(lane, now.row);
+        __syncwarp();
+        if (mine > 0) put_q(0, raw);
+    }
+#pragma unroll
+    for (int mt = 1; mt < MT; ++mt) {
+        uint2 raw[HN][8];
+        if (mine > 0) {
+            load_q(mt, raw);
+            put_q(mt, raw);
+        }
+    }
+    next = look(1);
 
     bool ok = true;
-    int i = 0;                                         // the key group's next stage
-    for (int s = s0; s < s1;) {
-        const Unit8 u = unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, s);
-        const int end = min(s1, u.first + u.stages);
-        const int rows_here = min(ROWS, u.n * a.G - u.tile * ROWS), row0 = u.tile * ROWS;
-
-        // ---- queries: halves of each row's own size ----
+    int i = 0, slot = 0;                               // the run's next stage
+    uint32_t parity = 0;
+    // o: transposed, [8-row tile][16 channels 16 c ..]: channels 16 c + 2 lrow (first two) and + 1, rows 2 quad and 2 quad + 1 of the tile; m, l: rows lrow
+    float o[NQ][8][4], m[NQ], l[NQ], ref_scale = 0.f;                  // ref_scale: the largest value scale so far
+    bool left = false;                                 // the unit at hand goes to the joint
+    while (i < mine) {
+        if (i > 0) {
+            u = unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, r0 + i);
 #pragma unroll
-        for (int r = tid >> 4; r < ROWS; r += kA8Threads / 16) {
-            uint4 raw = make_uint4(0u, 0u, 0u, 0u);
-            if (r < rows_here)
-                raw = reinterpret_cast<const uint4*>(a.q_rot + ((long)u.g * a.rows + (long)lens.new_off[u.b] * a.G + row0 + r) * 128)[tid & 15];
-            float x[8], most = 0.f;
-            to_floats<__nv_bfloat16, 8>(raw, x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]));
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-            int e = 14 - ((int)(__float_as_uint(most) >> 23) - 127);       // the row's maximum into [2^14, 2^15)
-            e = e > 100 ? 100 : e;
-            const float up = exp2_int(e);
-            uint32_t w[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = pack_f16x2(x[2 * k] * up, x[2 * k + 1] * up);
-            *reinterpret_cast<uint4*>(smem_gen + Plan::kQOff + r * kA8QStride + (tid & 15) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
-            if ((tid & 15) == 0) s_c[r] = a.scale_log2 * exp2_int(-e);
-        }
-        __syncthreads();
-
-        const uint8_t* q_at = smem_gen + Plan::kQOff + (rg * 16 * MT + lrow) * kA8QStride + quad * 8;
-        uint32_t qf[MT == 1 ? 8 : 1][4];               // one row tile: its queries stay in registers
-        auto q_frag = [&](int mt, int c, uint32_t (&f)[4]) {
-            const uint2 top = *reinterpret_cast<const uint2*>(q_at + mt * 16 * kA8QStride + c * 32);
-            const uint2 low = *reinterpret_cast<const uint2*>(q_at + (mt * 16 + 8) * kA8QStride + c * 32);
-            f[0] = top.x; f[1] = low.x; f[2] = top.y; f[3] = low.y;
-        };
-        if (MT == 1) {
-#pragma unroll
-            for (int c = 0; c < 8; ++c) q_frag(0, c, qf[MT == 1 ? c : 0]);
-        }
-        float factor[MT][2];
-        int last[MT][2];                               // the row's last key
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = rg * 16 * MT + mt * 16 + h * 8 + lrow;
-                factor[mt][h] = s_c[r];
-                last[mt][h] = r < rows_here ? u.L + (int)fast_div((uint32_t)(row0 + r), a.div_g) : u.L + u.n - 1;
+            for (int mt = 0; mt < MT; ++mt) {
+                uint2 raw[HN][8];
+                load_q(mt, raw);
+                put_q(mt, raw);
             }
-        float o[MT][16][4], m[MT][2], l[MT][2], ref_scale = 0.f;      // ref_scale: the largest value scale so far
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-            for (int t = 0; t < 16; ++t) o[mt][t][0] = o[mt][t][1] = o[mt][t][2] = o[mt][t][3] = 0.f;
-            m[mt][0] = m[mt][1] = -INFINITY;
-            l[mt][0] = l[mt][1] = 0.f;
         }
+        const int begin = r0 + i, end = min(r1, u.first + u.stages);
+        const int rows_here = u.n * a.G - u.tile * ROWS, row0 = u.tile * ROWS + rg * WROWS;      // this warp's rows: row0 ..
+        int last[NQ];                                  // the row's last key
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const int r = q * 8 + lrow;
+            last[q] = rg * WROWS + r < rows_here ? u.L + (int)fast_div((uint32_t)(row0 + r), a.div_g) : u.L + u.n - 1;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) o[q][c][0] = o[q][c][1] = o[q][c][2] = o[q][c][3] = 0.f;
+            m[q] = -INFINITY;
+            l[q] = 0.f;
+        }
+        ref_scale = 0.f;
 
-        for (; i < mine && s0 + kg + i * KG < end; ++i) {
+        for (; r0 + i < end; ++i) {
             if ((i & 31) == 0 && i > 0) {
                 now = next;
                 next = look((i >> 5) + 1);
             }
-            const int slot = i % SLOTS;
-            const uint32_t parity = (uint32_t)(i / SLOTS) & 1u;
-            const uint32_t kbase = ring + slot * kA8StageBytes, vbase = kbase + kA8StageBytes / 2;
+            const uint32_t kbase = (ring + slot * kA8StageBytes + lane * 128) ^ ((lane & 7) << 4), vbase = kbase + kA8StageBytes / 2;
             const float ks = __shfl_sync(0xffffffffu, now.ks, i & 31), vs = __shfl_sync(0xffffffffu, now.vs, i & 31);
-            const int key0 = (s0 + kg + i * KG - u.first) * kA8Keys;
+            const int key0 = (r0 + i - u.first) * kA8Keys;
             ok = ok && warp_wait(bar_full + 8 * slot, parity, kDevTimeoutMmaKV, a.status, s_abort, lane);
             if (ok) {
                 // ---- scores: 16 MT rows x 32 keys ----
@@ -254,17 +304,23 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
                     uint32_t kk[4], f[MT][4];
-                    ptx::ldmatrix_x4(kk, kbase + lane * 128 + (uint32_t)((c ^ (lane & 7)) << 4));
-                    if (MT == 1) {
+                    ptx::ldmatrix_x4(kk, kbase ^ (c << 4));
+                    if constexpr (NQ == 1) {
+                        f[0][0] = qf[c][0]; f[0][2] = qf[c][1]; f[0][1] = f[0][3] = 0u;       // (no rows in the lower half)
+                    } else if constexpr (Plan::kQRegs) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) f[0][e] = qf[MT == 1 ? c : 0][e];
+                        for (int e = 0; e < 4; ++e) f[0][e] = qf[c][e];
                     } else {
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) q_frag(mt, c, f[mt]);
+                        for (int mt = 0; mt < MT; ++mt) {
+                            const uint4 x = q_at[(mt * 8 + c) * 32];
+                            f[mt][0] = x.x; f[mt][1] = x.y; f[mt][2] = x.z; f[mt][3] = x.w;
+                        }
                     }
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
-                        const uint32_t b0 = halves2(kk[t]), b1 = halves2(kk[t] >> 16);
+                        uint32_t b0, b1;
+                        halves4(kk[t], b0, b1);
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt) mma_f16(sc[mt][t], f[mt], b0, b1);
                     }
@@ -274,81 +330,73 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                 const float shrink = grew ? ref_scale / vs : 1.f;
                 if (grew) ref_scale = vs;
                 const float ratio = fmaxf(log2f(vs / ref_scale), kA8LeastRatio) + kA8Lift, unlift = ptx::ex2(-ratio);
-                const bool masked = key0 + kA8Keys - 1 > u.L;
-                uint32_t p[MT][2][4];
+                if (key0 + kA8Keys - 1 > u.L) {                       // keys that not every row sees
+#pragma unroll
+                    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                        for (int t = 0; t < 4; ++t)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                if (key0 + 8 * t + 2 * quad + e > last[q]) sc[q >> 1][t][2 * (q & 1) + e] = -INFINITY;
+                }
+                uint32_t p[NQ][2][2];                                 // the transposed product's operand: two k-steps of 16 keys
                 bool moved = grew && shrink > 0.f;
-                float keep[MT][2];
+                float keep[NQ];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                for (int q = 0; q < NQ; ++q) {
+                    const int mt = q >> 1, h = q & 1;
+                    const float f = factor[mt][h] * ks;               // > 0
+                    float top = -INFINITY;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float f = factor[mt][h] * ks;
-                        float top = -INFINITY;
+                    for (int t = 0; t < 4; ++t) top = ptx::max3(top, sc[mt][t][2 * h], sc[mt][t][2 * h + 1]);
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * f;
+                    const bool move = top > m[q] + kA8Headroom;       // (from -inf: whenever there is a score)
+                    const float was = m[q];
+                    if (move) m[q] = top;
+                    const float alpha = move ? ptx::ex2(was - top) : 1.f;
+                    keep[q] = alpha * shrink;
+                    moved = moved || move;
+                    const float off = ratio - (m[q] == -INFINITY ? 0.f : m[q]);
+                    const uint64_t f2 = ptx::pack2(f, f), off2 = ptx::pack2(off, off);
+                    uint64_t sum2 = 0;
 #pragma unroll
-                        for (int t = 0; t < 4; ++t)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                float& x = sc[mt][t][2 * h + e];
-                                x *= f;
-                                if (masked && key0 + 8 * t + 2 * quad + e > last[mt][h]) x = -INFINITY;
-                                top = fmaxf(top, x);
-                            }
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                        const bool move = top > m[mt][h] + kA8Headroom;      // (from -inf: whenever there is a score)
-                        const float was = m[mt][h];
-                        if (move) m[mt][h] = top;
-                        const float alpha = move ? ptx::ex2(was - top) : 1.f;
-                        keep[mt][h] = alpha * shrink;
-                        moved = moved || move;
-                        const float off = ratio - (m[mt][h] == -INFINITY ? 0.f : m[mt][h]);
-                        float sum = 0.f;
-#pragma unroll
-                        for (int t = 0; t < 4; ++t)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                float& x = sc[mt][t][2 * h + e];
-                                x = ptx::ex2(x + off);
-                                sum += x;
-                            }
-                        l[mt][h] = fmaf(l[mt][h], alpha, sum * unlift);
+                    for (int t = 0; t < 4; ++t) {
+                        float x, y;
+                        ptx::unpack2(ptx::fma2(ptx::pack2(sc[mt][t][2 * h], sc[mt][t][2 * h + 1]), f2, off2), x, y);
+                        x = ptx::ex2(x);
+                        y = ptx::ex2(y);
+                        sum2 = ptx::add2(sum2, ptx::pack2(x, y));
+                        p[q][t >> 1][t & 1] = pack_f16x2(x, y);
                     }
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        p[mt][j][0] = pack_f16x2(sc[mt][2 * j][0], sc[mt][2 * j][1]);
-                        p[mt][j][1] = pack_f16x2(sc[mt][2 * j][2], sc[mt][2 * j][3]);
-                        p[mt][j][2] = pack_f16x2(sc[mt][2 * j + 1][0], sc[mt][2 * j + 1][1]);
-                        p[mt][j][3] = pack_f16x2(sc[mt][2 * j + 1][2], sc[mt][2 * j + 1][3]);
-                    }
+                    float x, y;
+                    ptx::unpack2(sum2, x, y);
+                    l[q] = fmaf(l[q], alpha, (x + y) * unlift);
+                }
                 if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                    for (int q = 0; q < NQ; ++q) {
+                        const float k0 = __shfl_sync(0xffffffffu, keep[q], 8 * quad), k1 = __shfl_sync(0xffffffffu, keep[q], 8 * quad + 4);   // rows 2 quad, 2 quad + 1
 #pragma unroll
-                        for (int t = 0; t < 16; ++t) {
-                            o[mt][t][0] *= keep[mt][0]; o[mt][t][1] *= keep[mt][0];
-                            o[mt][t][2] *= keep[mt][1]; o[mt][t][3] *= keep[mt][1];
+                        for (int c = 0; c < 8; ++c) {
+                            o[q][c][0] *= k0; o[q][c][1] *= k1;
+                            o[q][c][2] *= k0; o[q][c][3] *= k1;
                         }
+                    }
                 }
-                // ---- products with the values ----
+                // ---- products with the values, transposed: 16 channels down, 8 rows across ----
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
                     uint32_t vv[4], even[4], odd[4];
-                    ptx::ldmatrix_x4_trans(vv, vbase + lane * 128 + (uint32_t)((c ^ (lane & 7)) << 4));
+                    ptx::ldmatrix_x4_trans(vv, vbase ^ (c << 4));
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const uint32_t parted = __byte_perm(vv[t], 0, 0x3120);    // two keys of a channel, two of the next
-                        even[t] = halves2(parted);
-                        odd[t] = halves2(parted >> 16);
+                    for (int t = 0; t < 4; ++t) halves4(__byte_perm(vv[t], 0, 0x3120), even[t], odd[t]);    // two keys of a channel, two of the next
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t v[4] = {even[2 * j], odd[2 * j], even[2 * j + 1], odd[2 * j + 1]};
+#pragma unroll
+                        for (int q = 0; q < NQ; ++q) mma_f16(o[q][c], v, p[q][j][0], p[q][j][1]);
                     }
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-                            mma_f16(o[mt][2 * c], p[mt][j], even[2 * j], even[2 * j + 1]);
-                            mma_f16(o[mt][2 * c + 1], p[mt][j], odd[2 * j], odd[2 * j + 1]);
-                        }
                 }
             }
             // ---- the slot is read: the group's first warp refills it ----
@@ -358,134 +406,211 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                 const int ahead = i + SLOTS;
                 const int row = __shfl_sync(0xffffffffu, (ahead >> 5) == (i >> 5) ? now.row : next.row, ahead & 31);
                 if (RG > 1) ok = ok && warp_wait(bar_empty + 8 * slot, parity, kDevTimeoutProducer, a.status, s_abort, lane);
-                if (ok && lane == 0) load(ahead, row);
+                if (ok && lane == 0) load(slot, row);
+            }
+            if (++slot == SLOTS) {
+                slot = 0;
+                parity ^= 1u;
             }
         }
 
-        // ---- the key groups' results are joined: references and sums, then the outputs in turn ----
+        // ---- sums over the row's four lanes; a unit that this run ends is done here, whole or a part ----
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int q = 0; q < NQ; ++q) {
+            l[q] += __shfl_xor_sync(0xffffffffu, l[q], 1);
+            l[q] += __shfl_xor_sync(0xffffffffu, l[q], 2);
+        }
+        const bool whole = begin == u.first && end == u.first + u.stages;
+        left = !whole && end == r1;
+        if (!left) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float sum = l[mt][h];
-                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                const int r = rg * 16 * MT + mt * 16 + h * 8 + lrow;
-                if (quad == 0) {
-                    s_m[kg * ROWS + r] = m[mt][h];
-                    s_l[kg * ROWS + r] = sum;
-                }
-            }
-        __syncthreads();
+            for (int q = 0; q < NQ; ++q) {
+                const float by_row = l[q] == 0.f ? 0.f : ref_scale * exp2_int(-(int)kA8Lift) / l[q], lse_row = l[q] == 0.f ? -INFINITY : m[q] + log2f(l[q]);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+                for (int e = 0; e < 2; ++e) {
+                    const float by = __shfl_sync(0xffffffffu, by_row, 8 * quad + 4 * e), lse2 = __shfl_sync(0xffffffffu, lse_row, 8 * quad + 4 * e);
+                    const int r = q * 8 + 2 * quad + e;
+                    if (rg * WROWS + r >= rows_here) continue;
+                    if (whole) {
+                        const long at = out_row8(a, lens, u, row0 + r);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = rg * 16 * MT + mt * 16 + h * 8 + lrow;
-                float top = -INFINITY;
+                        for (int c = 0; c < 8; ++c) reinterpret_cast<uint32_t*>(a.out + at * 128)[8 * c + lrow] = ptx::pack_bf16x2(o[q][c][e] * by, o[q][c][2 + e] * by);
+                        if (a.lse_out && lrow == 0) a.lse_out[at] = lse2 * kLn2;
+                    } else {
+                        const long at = 2L * run * ROWS + rg * WROWS + r;
 #pragma unroll
-                for (int k = 0; k < KG; ++k) top = fmaxf(top, s_m[k * ROWS + r]);
-                const float w = m[mt][h] == -INFINITY ? 0.f : ptx::ex2(m[mt][h] - top) * ref_scale * exp2_int(-(int)kA8Lift);
-#pragma unroll
-                for (int t = 0; t < 16; ++t) {
-                    o[mt][t][2 * h] *= w;
-                    o[mt][t][2 * h + 1] *= w;
-                }
-            }
-        for (int turn = 0; turn < KG / Plan::kBufs; ++turn) {
-            if (kg / Plan::kBufs == turn) {
-                float* buf = s_o + (kg % Plan::kBufs) * ROWS * kA8OStride;
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float4* to = reinterpret_cast<float4*>(buf + (rg * 16 * MT + mt * 16 + h * 8 + lrow) * kA8OStride + quad * 4);
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            float4 x = make_float4(o[mt][2 * c][2 * h], o[mt][2 * c + 1][2 * h], o[mt][2 * c][2 * h + 1], o[mt][2 * c + 1][2 * h + 1]);
-                            if (turn > 0) {
-                                const float4 y = to[4 * c];
-                                x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-                            }
-                            to[4 * c] = x;
-                        }
+                        for (int c = 0; c < 8; ++c) reinterpret_cast<float2*>(a.o_part + at * 128)[8 * c + lrow] = make_float2(o[q][c][e] * by, o[q][c][2 + e] * by);
+                        if (lrow == 0) a.lse_part[at] = lse2;
                     }
-            }
-            __syncthreads();
-        }
-        const bool whole = s == u.first && end == u.first + u.stages;
-        const long part = 2L * blockIdx.x + (u.first <= s0 ? 0 : 1);
-        for (int r = tid >> 4; r < rows_here; r += kA8Threads / 16) {
-            float top = -INFINITY, sum = 0.f;
-#pragma unroll
-            for (int k = 0; k < KG; ++k) top = fmaxf(top, s_m[k * ROWS + r]);
-#pragma unroll
-            for (int k = 0; k < KG; ++k) sum += s_m[k * ROWS + r] == -INFINITY ? 0.f : s_l[k * ROWS + r] * ptx::ex2(s_m[k * ROWS + r] - top);
-            const float inv = sum > 0.f ? 1.f / sum : 0.f, lse2 = sum > 0.f ? top + log2f(sum) : -INFINITY;
-            const bool nan = !(sum >= 0.f);            // undefined scores: an undefined row
-            const int c0 = (tid & 15) * 8;
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-                const float4 y = *reinterpret_cast<const float4*>(s_o + r * kA8OStride + c0 + e);
-                const float4 z = *reinterpret_cast<const float4*>(s_o + (ROWS + r) * kA8OStride + c0 + e);
-                x[e] = (y.x + z.x) * inv; x[e + 1] = (y.y + z.y) * inv; x[e + 2] = (y.z + z.z) * inv; x[e + 3] = (y.w + z.w) * inv;
-            }
-            if (nan) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = sum;
-            }
-            if (whole) {
-                const int rl = row0 + r, tok = (int)fast_div((uint32_t)rl, a.div_g);
-                const long at = ((long)lens.new_off[u.b] + tok) * (a.Hkv * a.G) + u.g * a.G + (rl - tok * a.G);
-                *reinterpret_cast<uint4*>(a.out + at * 128 + c0) = from_floats<__nv_bfloat16, 8>(x);
-                if (a.lse_out && c0 == 0) a.lse_out[at] = nan ? sum : lse2 * 0.69314718055994531f;
-            } else {
-                float4* to = reinterpret_cast<float4*>(a.o_part + (part * ROWS + r) * 128 + c0);
-                to[0] = make_float4(x[0], x[1], x[2], x[3]);
-                to[1] = make_float4(x[4], x[5], x[6], x[7]);
-                if (c0 == 0) a.lse_part[part * ROWS + r] = nan ? sum : lse2;
+                }
             }
         }
-        __syncthreads();
-        s = end;
     }
-    if (*s_abort && lane == 0) {
+
+    // ---- the joint: runs of the block that ended in the same unit ----
+    if (rg == 0 && lane == 0) s_unit[kg] = left ? u.first : -1;
+    if (left && quad == 0) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            s_m[warp * WROWS + q * 8 + lrow] = m[q];
+            s_l[warp * WROWS + q * 8 + lrow] = l[q];
+        }
+    }
+    __syncthreads();                                   // (every load has been waited for: the rings are free)
+    if (*s_abort) {
         const long long t0 = clock64();                // loads in flight land before the block may leave
         while (clock64() - t0 < 400000) { }
+        return;
+    }
+    float* s_o = reinterpret_cast<float*>(smem_gen);   // [warp][WROWS][kA8OStride]
+    float top[NQ];
+    if (left) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            top[q] = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < KG; ++k)
+                if (s_unit[k] == u.first) top[q] = fmaxf(top[q], s_m[(k * RG + rg) * WROWS + q * 8 + lrow]);
+            const float w = m[q] == -INFINITY ? 0.f : ptx::ex2(m[q] - top[q]), by_row = w * ref_scale * exp2_int(-(int)kA8Lift);
+            l[q] = l[q] == 0.f ? 0.f : l[q] * w;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float by = __shfl_sync(0xffffffffu, by_row, 8 * quad + 4 * e);
+                float2* to = reinterpret_cast<float2*>(s_o + (warp * WROWS + q * 8 + 2 * quad + e) * kA8OStride) + lrow;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) to[8 * c] = make_float2(o[q][c][e] * by, o[q][c][2 + e] * by);
+            }
+        }
+    }
+    __syncthreads();                                   // (the references are read)
+    if (left && quad == 0) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            s_m[warp * WROWS + q * 8 + lrow] = top[q];
+            s_l[warp * WROWS + q * 8 + lrow] = l[q];
+        }
+    }
+    __syncthreads();
+    for (int k0 = 0; k0 < KG;) {
+        const int at_unit = s_unit[k0];
+        int k1 = k0 + 1;
+        while (k1 < KG && s_unit[k1] == at_unit) ++k1;
+        if (at_unit >= 0) {
+            const Unit8 w = left && u.first == at_unit ? u : unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, at_unit);
+            const int first_run = blockIdx.x * KG + k0, ends = min(a.total, (blockIdx.x * KG + k1) * a.run);
+            const bool whole = first_run * a.run <= w.first && ends == w.first + w.stages;
+            const int rows_here = min(ROWS, w.n * a.G - w.tile * ROWS);
+            for (int r = tid >> 5; r < rows_here; r += Plan::kWarps) {               // a warp per row, four channels a lane
+                const int at0 = (k0 * RG + r / WROWS) * WROWS + r % WROWS;
+                float sum = 0.f;
+                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int k = 0; k < KG; ++k) {
+                    if (k0 + k >= k1) continue;
+                    const int at = at0 + k * RG * WROWS;
+                    const float4 y = *reinterpret_cast<const float4*>(s_o + at * kA8OStride + 4 * lane);
+                    sum += s_l[at];
+                    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                }
+                const float by = sum == 0.f ? 0.f : 1.f / sum, lse2 = sum == 0.f ? -INFINITY : s_m[at0] + log2f(sum);
+                x.x *= by; x.y *= by; x.z *= by; x.w *= by;
+                if (whole) {
+                    const long at = out_row8(a, lens, w, w.tile * ROWS + r);
+                    reinterpret_cast<uint2*>(a.out + at * 128)[lane] = make_uint2(ptx::pack_bf16x2(x.x, x.y), ptx::pack_bf16x2(x.z, x.w));
+                    if (a.lse_out && lane == 0) a.lse_out[at] = lse2 * kLn2;
+                } else {
+                    const long at = (2L * first_run + 1) * ROWS + r;
+                    reinterpret_cast<float4*>(a.o_part + at * 128)[lane] = x;
+                    if (lane == 0) a.lse_part[at] = lse2;
+                }
+            }
+        }
+        k0 = k1;
     }
 }
 
-// Joins the parts of the units that the blocks' shares cut: a warp per row.  grid (blocks - 1, warps of rows): block x serves the
-// unit that the start of share x + 1 lies in, if no earlier start does.
-template <int ROWS>
+// The units that merge8_kernel looks at: all of the batch's where they are few, by the stages before them; else (count 0) block x takes
+// those that begin in block x's share of the attention kernel.
+constexpr int kMergeUnits = 192;
+struct MergeList {
+    int count;
+    int first[kMergeUnits];
+};
+
+// Joins the parts of the units that the runs cut: what each block's runs that end in the unit left jointly, and what a run left that goes on
+// behind its end.  Blocks (x, y): units as in MergeList, rows y, y + gridDim.y, ...; the four warps share a row's parts.
+// Blocks without such a unit leave at once (the first one does not: the next kernel in the stream waits for this grid, which
+// therefore must not end before the attention kernel has), so the others are on the SMs, and know what to read, when the parts are there.
+template <int ROWS, int KG>
 __global__ void __launch_bounds__(128)
-merge8_kernel(const Attn8Args a, const __grid_constant__ BatchLens lens)
+merge8_kernel(const Attn8Args a, const __grid_constant__ BatchLens lens, const __grid_constant__ MergeList list)
 {
-    const int lane = threadIdx.x & 31, i0 = blockIdx.x, cut = (i0 + 1) * a.share;
-    const Unit8 u = unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, cut);
+    __shared__ float4 s_x[4][32];
+    __shared__ float s_sum[4];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Unit8 u;
+    int u1, ra, rb;
+    bool on;                                           // the unit's last run goes on behind it
+    auto cut = [&](int first) -> bool {
+        u = unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, first);
+        u1 = u.first + u.stages;
+        ra = u.first / a.run;
+        rb = (u1 - 1) / a.run;
+        on = min(a.total, (rb + 1) * a.run) > u1;
+        return ra != rb && (on || ra / KG != rb / KG); // else whole: in one run, or in the joint of one block
+    };
+    int next, to;
+    if (list.count > 0) {
+        next = list.first[blockIdx.x];
+        to = next + 1;
+    } else {
+        next = blockIdx.x * KG * a.run;
+        to = min(a.total, next + KG * a.run);
+        u = unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, next);
+        if (u.first < next) next = u.first + u.stages;
+    }
+    bool found = false;
+    while (next < to && !(found = cut(next))) next = u1;
+    if (!found && (blockIdx.x > 0 || blockIdx.y > 0)) return;
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    const int r = blockIdx.y * 4 + (threadIdx.x >> 5), rl = u.tile * ROWS + r;
-    if (u.first == cut || u.first < i0 * a.share || rl >= u.n * a.G) return;
-    const int i1 = (u.first + u.stages - 1) / a.share;
-    float top = -INFINITY, sum = 0.f;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = i0; i <= i1; ++i) {
-        const long part = 2L * i + (u.first <= i * a.share ? 0 : 1);
-        const float lse = a.lse_part[part * ROWS + r];
-        if (lse == -INFINITY) continue;                // no key of the row in this part
-        const float4 y = reinterpret_cast<const float4*>(a.o_part + (part * ROWS + r) * 128)[lane];
-        const float up = fmaxf(top, lse), was = ptx::ex2(top - up), is = ptx::ex2(lse - up);
-        top = up;
-        sum = fmaf(sum, was, is);
-        x.x = fmaf(x.x, was, y.x * is); x.y = fmaf(x.y, was, y.y * is); x.z = fmaf(x.z, was, y.z * is); x.w = fmaf(x.w, was, y.w * is);
+    while (found) {
+        const int b0 = ra / KG, joints = (on ? rb - 1 : rb) / KG - b0 + 1, parts = joints + (on ? 1 : 0);
+        auto row_of = [&](int p, int r) -> long { return (p < joints ? 2L * max(ra, (b0 + p) * KG) + 1 : 2L * rb) * ROWS + r; };
+        for (int r = blockIdx.y; r < min(ROWS, u.n * a.G - u.tile * ROWS); r += gridDim.y) {
+            float top = -INFINITY, sum = 0.f;
+            for (int p = lane; p < parts; p += 32) top = fmaxf(top, a.lse_part[row_of(p, r)]);
+#pragma unroll
+            for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+            for (int p = warp; p < parts; p += 4) {
+                const long at = row_of(p, r);
+                const float4 y = reinterpret_cast<const float4*>(a.o_part + at * 128)[lane];
+                const float w = ptx::ex2(a.lse_part[at] - top);      // 0: no key of the row in this part
+                sum += w;
+                x.x = fmaf(y.x, w, x.x); x.y = fmaf(y.y, w, x.y); x.z = fmaf(y.z, w, x.z); x.w = fmaf(y.w, w, x.w);
+            }
+            s_x[warp][lane] = x;
+            if (lane == 0) s_sum[warp] = sum;
+            __syncthreads();
+            if (warp == 0) {
+                for (int w = 1; w < 4; ++w) {
+                    const float4 y = s_x[w][lane];
+                    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                    sum += s_sum[w];
+                }
+                const float by = 1.f / sum;
+                const long at = out_row8(a, lens, u, u.tile * ROWS + r);
+                reinterpret_cast<uint2*>(a.out + at * 128)[lane] = make_uint2(ptx::pack_bf16x2(x.x * by, x.y * by), ptx::pack_bf16x2(x.z * by, x.w * by));
+                if (a.lse_out && lane == 0) a.lse_out[at] = (top + log2f(sum)) * kLn2;
+            }
+            __syncthreads();
+        }
+        next = u1;
+        found = false;
+        while (next < to && !(found = cut(next))) next = u1;
     }
-    const float inv = 1.f / sum;
-    const int tok = (int)fast_div((uint32_t)rl, a.div_g);
-    const long at = ((long)lens.new_off[u.b] + tok) * (a.Hkv * a.G) + u.g * a.G + (rl - tok * a.G);
-    reinterpret_cast<uint2*>(a.out + at * 128)[lane] = make_uint2(ptx::pack_bf16x2(x.x * inv, x.y * inv), ptx::pack_bf16x2(x.z * inv, x.w * inv));
-    if (a.lse_out && lane == 0) a.lse_out[at] = (top + log2f(sum)) * 0.69314718055994531f;
 }
 
 }  // namespace evln

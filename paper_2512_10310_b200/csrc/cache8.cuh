@@ -64,16 +64,15 @@ __device__ __forceinline__ uint2 codes8(const float (&x)[8], float inv)
 {
     return make_uint2(codes4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv), codes4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv));
 }
-// two codes to two halves, exactly (NaN stays NaN)
-__device__ __forceinline__ uint32_t halves2(uint32_t two_codes)
+// four codes to four halves, exactly (NaN stays NaN)
+__device__ __forceinline__ void halves4(uint32_t codes, uint32_t& lo, uint32_t& hi)
 {
-    uint32_t r;
-    asm("{\n\t.reg .b16 t, u;\n\tmov.b32 {t, u}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, t;\n\t}" : "=r"(r) : "r"(two_codes));
-    return r;
+    asm("{\n\t.reg .b16 t, u;\n\tmov.b32 {t, u}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, t;\n\tcvt.rn.f16x2.e4m3x2 %1, u;\n\t}" : "=r"(lo), "=r"(hi) : "r"(codes));
 }
 __device__ __forceinline__ void floats4(uint32_t codes, float* x)
 {
-    const uint32_t lo = halves2(codes), hi = halves2(codes >> 16);
+    uint32_t lo, hi;
+    halves4(codes, lo, hi);
     const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo));
     const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
     x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;

@@ -26,7 +26,8 @@ cudaError_t prepare_cache_kernels()
 {
     const std::pair<const void*, int> kernels[] = {{(const void*)attn8_kernel<1, 1>, Attn8Plan<1, 1>::kBytes},
                                                    {(const void*)attn8_kernel<2, 1>, Attn8Plan<2, 1>::kBytes},
-                                                   {(const void*)attn8_kernel<2, 2>, Attn8Plan<2, 2>::kBytes},
+                                                   {(const void*)attn8_kernel<4, 1>, Attn8Plan<4, 1>::kBytes},
+                                                   {(const void*)attn8_kernel<4, 2>, Attn8Plan<4, 2>::kBytes},
                                                    {(const void*)key_weights_kernel<64>, KeyWeightPlan<64>::kBytes},
                                                    {(const void*)key_weights_kernel<128>, KeyWeightPlan<128>::kBytes},
                                                    {(const void*)select_keys_kernel, kSelectCache * 4}};
@@ -110,8 +111,8 @@ constexpr int kA8MostRows = 256;
 
 struct Plan8 {
     bool expand;
-    int rows;                // of a tile: 16, 32 or 64
-    int share, total, blocks;
+    int most, rows;          // query rows of the longest episode (per kv head), of a tile: 8, 16, 32 or 64
+    int run, total, runs, blocks;        // stages of a run, of the batch; runs, blocks
     int pages;               // expand: pages of the copy
     size_t copy_bytes;       // expand: table and pools
 };
@@ -128,8 +129,9 @@ evlnStatus_t plan8(evlnHandle_t h, const evlnPagedParams* p, const int* lens, co
     long most = 0, total = 0, pages = 0;
     for_episodes(p, lens, offs, [&](int, int, int n) { if ((long)n * G > most) most = (long)n * G; });
     *pl = Plan8();
+    pl->most = (int)most;
     pl->expand = most > kA8MostRows;
-    pl->rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+    pl->rows = most <= 8 ? 8 : most <= 16 ? 16 : most <= 32 ? 32 : 64;
     for_episodes(p, lens, offs, [&](int, int L, int n) {
         if (n == 0) return;
         pages += ((long)L + n + kPage8 - 1) / kPage8;
@@ -141,15 +143,18 @@ evlnStatus_t plan8(evlnHandle_t h, const evlnPagedParams* p, const int* lens, co
         pl->copy_bytes = round_up((size_t)p->batch * p->max_pages_per_seq * sizeof(int), 1024) + (size_t)pages * p->num_kv_heads * kPage8 * 128 * 2 * 2;
         return EVLN_OK;
     }
-    // an SM each, but at least a stage for every warp of a block
+    // the SMs' key groups each a run of the same length
+    const int groups = pl->rows == 8 ? Attn8Plan<1, 1>::kKeyGroups : pl->rows == 16 ? Attn8Plan<2, 1>::kKeyGroups
+                     : pl->rows == 32 ? Attn8Plan<4, 1>::kKeyGroups : Attn8Plan<4, 2>::kKeyGroups;
     pl->total = (int)total;
-    pl->share = ceil_div(pl->total, h->num_sms);
-    if (pl->share < kA8Warps) pl->share = kA8Warps;
-    pl->blocks = ceil_div(pl->total, pl->share);
+    pl->run = ceil_div(pl->total, h->num_sms * groups);
+    if (pl->run < 1) pl->run = 1;
+    pl->runs = ceil_div(pl->total, pl->run);
+    pl->blocks = ceil_div(pl->runs, groups);
     return EVLN_OK;
 }
 
-size_t part_bytes8(const Plan8& pl) { return round_up((size_t)2 * pl.blocks * pl.rows * (128 + 1) * sizeof(float), 256); }
+size_t part_bytes8(const Plan8& pl) { return round_up((size_t)2 * pl.runs * pl.rows * (128 + 1) * sizeof(float), 256); }
 
 // The paged call that serves the bf16 copy.
 evlnPagedParams copy_params(const evlnPagedParams* p, const Plan8& pl)
@@ -159,13 +164,25 @@ evlnPagedParams copy_params(const evlnPagedParams* p, const Plan8& pl)
     return c;
 }
 
-template <int MT, int RG>
-cudaError_t launch_attn8(const Plan8& pl, cudaStream_t st, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Attn8Args& a, const BatchLens& bl)
+template <int NQ, int RG>
+cudaError_t launch_attn8(const Plan8& pl, int most_rows, cudaStream_t st, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Attn8Args& a, const BatchLens& bl)
 {
-    using Plan = Attn8Plan<MT, RG>;
-    cudaError_t e = launch_pdl(attn8_kernel<MT, RG>, dim3(pl.blocks), dim3(kA8Threads), Plan::kBytes, st, tm_k, tm_v, a, bl);
-    if (e == cudaSuccess && pl.blocks > 1)
-        e = launch_pdl(merge8_kernel<Plan::kRows>, dim3(pl.blocks - 1, Plan::kRows / 4), dim3(128), 0, st, a, bl);
+    using Plan = Attn8Plan<NQ, RG>;
+    cudaError_t e = launch_pdl(attn8_kernel<NQ, RG>, dim3(pl.blocks), dim3(Plan::kThreads), Plan::kBytes, st, tm_k, tm_v, a, bl);
+    if (e == cudaSuccess && pl.runs > 1) {
+        MergeList list = {};
+        for (int b = 0; b < a.batch && list.count <= kMergeUnits; ++b) {
+            const int n = bl.new_off[b + 1] - bl.new_off[b];
+            if (n == 0) continue;
+            const int stages = ceil_div(bl.cache_len[b] + n, kA8Keys), units = (bl.item_off[b + 1] - bl.item_off[b]) / stages;
+            for (int i = 0; i < units && list.count <= kMergeUnits; ++i, ++list.count)
+                if (list.count < kMergeUnits) list.first[list.count] = bl.item_off[b] + i * stages;
+        }
+        const bool few = list.count <= kMergeUnits;
+        if (!few) list.count = 0;
+        const int rows = most_rows < Plan::kRows ? most_rows : Plan::kRows;
+        e = launch_pdl(merge8_kernel<Plan::kRows, Plan::kKeyGroups>, dim3(few ? list.count : pl.blocks, few || rows < 16 ? rows : 16), dim3(128), 0, st, a, bl, list);
+    }
     return e;
 }
 
@@ -347,15 +364,16 @@ evlnStatus_t evlnPaged8StepAttention(evlnHandle_t h, const evlnPagedParams* p, c
     a.page_table = d_page_table;
     a.out = (__nv_bfloat16*)out; a.lse_out = lse_out;
     a.o_part = (float*)workspace;
-    a.lse_part = a.o_part + (size_t)2 * pl.blocks * pl.rows * 128;
+    a.lse_part = a.o_part + (size_t)2 * pl.runs * pl.rows * 128;
     a.status = h->d_status;
     a.Hkv = hkv; a.G = G; a.rows = total * G; a.batch = p->batch; a.max_pages = p->max_pages_per_seq;
-    a.share = pl.share; a.total = pl.total;
+    a.run = pl.run; a.total = pl.total;
     a.scale_log2 = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf(128.f)) * 1.4426950408889634f;
     a.div_g = make_fast_div((uint32_t)G);
-    return launched(h, pl.rows == 16   ? launch_attn8<1, 1>(pl, st, tm_k, tm_v, a, bl)
-                       : pl.rows == 32 ? launch_attn8<2, 1>(pl, st, tm_k, tm_v, a, bl)
-                                       : launch_attn8<2, 2>(pl, st, tm_k, tm_v, a, bl));
+    return launched(h, pl.rows == 8    ? launch_attn8<1, 1>(pl, pl.most, st, tm_k, tm_v, a, bl)
+                       : pl.rows == 16 ? launch_attn8<2, 1>(pl, pl.most, st, tm_k, tm_v, a, bl)
+                       : pl.rows == 32 ? launch_attn8<4, 1>(pl, pl.most, st, tm_k, tm_v, a, bl)
+                                       : launch_attn8<4, 2>(pl, pl.most, st, tm_k, tm_v, a, bl));
 }
 
 // ---- eviction --------------------------------------------------------------------------------
