@@ -7,9 +7,8 @@
 // token arrives: codes that stay normal numbers only change their exponents, so no error piles up.
 //
 // append8_kernel: a block for every (touched page, kv head, keys or values), and blocks for the tokens' queries.  A page
-// block holds its new tokens (8 lanes a token, 16 channels a lane, two tokens a thread) in registers from the load over
-// norm, rotation and the block's maximum to the codes: one pass.  Codes of earlier tokens are loaded beside them and stored
-// again only if the scale grew.
+// block holds its tokens (8 lanes a token, 16 channels a lane) in registers from the load over norm, rotation and the block's
+// maximum to the codes: one pass.  Codes of earlier tokens are loaded instead of new ones and stored again only if the scale grew.
 // Bound: latency for a token an episode (a chain of loads, the block's maximum, stores), else the queries' traffic.
 #pragma once
 
@@ -22,7 +21,8 @@
 
 namespace evln {
 
-constexpr int kPage8 = 64, kAppend8Threads = 256;
+constexpr int kPage8 = 64, kAppend8Threads = 8 * kPage8;
+constexpr int kAppend8Tokens = 16;                     // most tokens of a query block
 constexpr int kScaleMin8 = -120, kScaleMax8 = 120;     // exponents; a page of zeros has the least scale
 
 struct Append8Args {
@@ -31,8 +31,9 @@ struct Append8Args {
     float* k_scale;          // [pages, Hkv]
     float* v_scale;
     int page_blocks;         // touched pages * Hkv
-    int q_parts;             // blocks per token for its queries
-    FastDiv div_hkv, div_parts;
+    int q_threads;           // threads per token for its queries (whole warps); a block takes kAppend8Threads / q_threads tokens
+    int q_tokens;            // ... of them
+    FastDiv div_hkv;
 };
 
 __device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
@@ -79,141 +80,137 @@ __device__ __forceinline__ void floats4(uint32_t codes, float* x)
 }
 
 template <bool NORM>
-__global__ void __launch_bounds__(kAppend8Threads)
+__global__ void __launch_bounds__(kAppend8Threads, 2)
 append8_kernel(const Append8Args p, const __grid_constant__ BatchLens lens)
 {
     typedef __nv_bfloat16 T;
-    constexpr int D = 128, half = 64;
+    constexpr int D = 128, half = 64, kVectors = 8;        // vector pairs of a head
+    __shared__ __align__(16) TokenAngles<T, NORM> s_angles[kAppend8Tokens];
+    __shared__ float s_most[kAppend8Threads / 32];
     const RopeArgs& a = p.r;
-    const int blk = blockIdx.x;
-    int b = 0, hi = a.batch;
+    const int blk = blockIdx.x, k = threadIdx.x & (kVectors - 1), c0 = k * 8;      // a lane's channels: c0 .. and c0 + 64 ..
     if (blk >= 2 * p.page_blocks) {
-        // ---- a token's queries ----
-        const int at = blk - 2 * p.page_blocks, tok = (int)fast_div((uint32_t)at, p.div_parts), part = at - tok * p.q_parts;
-        while (hi - b > 1) {                              // largest b with new_off[b] <= tok
-            const int mid = (b + hi) >> 1;
-            if (lens.new_off[mid] <= tok) b = mid; else hi = mid;
-        }
-        const int pos = lens.cache_len[b] + tok - lens.new_off[b];
-        const double omega = !a.table && (int)threadIdx.x < half ? rope_omega(threadIdx.x, D, a.log2_theta) : 0.0;
+        // ---- queries of a few tokens ----
+        const int tok0 = (blk - 2 * p.page_blocks) * p.q_tokens, tokens = min(p.q_tokens, a.num_new - tok0);
+        auto position = [&](int tok) -> int {
+            int b = 0, hi = a.batch;                          // largest b with new_off[b] <= tok
+            while (hi - b > 1) {
+                const int mid = (b + hi) >> 1;
+                if (lens.new_off[mid] <= tok) b = mid; else hi = mid;
+            }
+            return lens.cache_len[b] + tok - lens.new_off[b];
+        };
+        const double omega = a.table ? 0.0 : rope_omega(threadIdx.x & (half - 1), D, a.log2_theta);
+        const int group = threadIdx.x / p.q_threads, tok = tok0 + group, items = a.Hq * kVectors;
         ptx::grid_dependency_wait();
         ptx::grid_launch_dependents();
-        norm_token<T, NORM, false>(
-            a, p.norm, tok, part, p.q_parts,
-            [&](int h) -> T* {
-                const int g = (int)fast_div((uint32_t)h, a.div_g);
-                return (T*)a.q_rot + ((long)g * a.num_new * a.G + (long)tok * a.G + (h - g * a.G)) * D;
-            },
-            [](int) -> T* { return nullptr; }, [](int) -> T* { return nullptr; },
-            [&](int j) -> double2 { return a.table ? a.table[(long)(pos - a.table_first) * half + j] : rope_cos_sin_at(pos, omega); });
+        int it = threadIdx.x - group * p.q_threads;
+        const bool there = group < tokens;
+        const T* src = (const T*)a.q_new + tok * a.q_stride + c0;
+        uint4 r0 = make_uint4(0u, 0u, 0u, 0u), r1 = r0;
+        auto load = [&]() {
+            if (there && it < items) {
+                r0 = *reinterpret_cast<const uint4*>(src + (it / kVectors) * D);
+                r1 = *reinterpret_cast<const uint4*>(src + (it / kVectors) * D + half);
+            }
+        };
+        load();                                               // in flight while the angles arrive
+        for (int e = threadIdx.x; e < tokens * half; e += kAppend8Threads) {
+            const int j = e & (half - 1), pos = position(tok0 + e / half);
+            s_angles[e / half].put(j, a.table ? a.table[(long)(pos - a.table_first) * half + j] : rope_cos_sin_at(pos, omega));
+        }
+        __syncthreads();
+        if (!there) return;                                   // (whole warps)
+        for (; it - (int)(threadIdx.x & 31) < items; it += p.q_threads, load()) {
+            uint4 y0, y1;
+            if constexpr (NORM) norm_turn<T>(s_angles[group], k, 3, D, p.norm.eps, (const T*)p.norm.q_weight, r0, r1, y0, y1);
+            else Rotation<T>::turn(s_angles[group].at, k, r0, r1, y0, y1);
+            if (it >= items) continue;
+            const int h = it / kVectors, g = (int)fast_div((uint32_t)h, a.div_g);
+            T* dst = (T*)a.q_rot + ((long)g * a.num_new * a.G + (long)tok * a.G + (h - g * a.G)) * D + c0;
+            *reinterpret_cast<uint4*>(dst) = y0;
+            *reinterpret_cast<uint4*>(dst + half) = y1;
+        }
         return;
     }
     // ---- a page of one kv head: keys (first, they have the longer chain) or values ----
     const bool is_v = blk >= p.page_blocks;
     const int item = is_v ? blk - p.page_blocks : blk;
     const int pg = (int)fast_div((uint32_t)item, p.div_hkv), g = item - pg * a.Hkv;
+    int b = 0, hi = a.batch;
     while (hi - b > 1) {                                  // largest b with item_off[b] <= pg: touched pages before an episode's
         const int mid = (b + hi) >> 1;
         if (lens.item_off[mid] <= pg) b = mid; else hi = mid;
     }
     const int L = lens.cache_len[b], off = lens.new_off[b], n = lens.new_off[b + 1] - off;
     const int p0 = (L / kPage8 + pg - lens.item_off[b]) * kPage8;          // position of the page's first slot
-    const int lane8 = threadIdx.x & 7, slot0 = threadIdx.x >> 3;           // slots slot0, slot0 + 32
-    const int c0 = lane8 * 8;                                              // channels c0.., c0 + 64..
-    __shared__ float s_most[kAppend8Threads / 32];
+    const int slot = threadIdx.x / kVectors, pos = p0 + slot;
+    const bool is_old = pos < L, is_new = pos >= L && pos < L + n, held = p0 < L;
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     const int page = a.page_table[(long)b * a.max_pages + p0 / kPage8];
-    uint8_t* pool = (uint8_t*)(is_v ? a.v_cache : a.k_cache) + ((long)page * a.Hkv + g) * (kPage8 * D);
+    uint8_t* at = (uint8_t*)(is_v ? a.v_cache : a.k_cache) + (((long)page * a.Hkv + g) * kPage8 + slot) * D + c0;
     float* scale_at = (is_v ? p.v_scale : p.k_scale) + (long)page * a.Hkv + g;
-    const bool held = p0 < L;
 
-    uint4 raw[2][2];
-    uint2 old[2][2];
-    bool is_new[2], is_old[2];
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        const int pos = p0 + slot0 + 32 * r;
-        is_old[r] = pos < L;
-        is_new[r] = pos >= L && pos < L + n;
-        raw[r][0] = raw[r][1] = make_uint4(0u, 0u, 0u, 0u);
-        if (is_new[r]) {
-            const long tok = off + pos - L;
-            const T* src = (is_v ? (const T*)a.v_new + tok * a.v_stride : (const T*)a.k_new + tok * a.k_stride) + (long)g * D + c0;
-            raw[r][0] = *reinterpret_cast<const uint4*>(src);
-            raw[r][1] = *reinterpret_cast<const uint4*>(src + half);
-        }
-        if (is_old[r]) {
-            const uint8_t* at = pool + (slot0 + 32 * r) * D + c0;
-            old[r][0] = *reinterpret_cast<const uint2*>(at);
-            old[r][1] = *reinterpret_cast<const uint2*>(at + half);
-        }
+    uint4 r0 = make_uint4(0u, 0u, 0u, 0u), r1 = r0;       // a new token's 16 numbers, or an earlier one's 16 codes
+    if (is_new) {
+        const long tok = off + pos - L;
+        const T* src = (is_v ? (const T*)a.v_new + tok * a.v_stride : (const T*)a.k_new + tok * a.k_stride) + (long)g * D + c0;
+        r0 = *reinterpret_cast<const uint4*>(src);
+        r1 = *reinterpret_cast<const uint4*>(src + half);
+    } else if (is_old) {
+        const uint2 lo = *reinterpret_cast<const uint2*>(at), hi8 = *reinterpret_cast<const uint2*>(at + half);
+        r0 = make_uint4(lo.x, lo.y, hi8.x, hi8.y);
     }
     const float old_scale = held ? *scale_at : 0.f;
-    uint4 w0 = make_uint4(0u, 0u, 0u, 0u), w1 = w0;
-    if (NORM && !is_v && p.norm.k_weight) {
-        w0 = *reinterpret_cast<const uint4*>((const T*)p.norm.k_weight + c0);
-        w1 = *reinterpret_cast<const uint4*>((const T*)p.norm.k_weight + c0 + half);
-    }
-    float x[2][2][8];
-    float most = 0.f;
+    float x[2][8], most = 0.f;
+    float inv = 1.f;
+    if (NORM && !is_v) inv = norm_factor<T>(r0, r1, 3, D, p.norm.eps);
+    if (is_new) {
+        to_floats<T, 8>(r0, x[0]);
+        to_floats<T, 8>(r1, x[1]);
+        if (!is_v) {
+            if (NORM) {
+                const T* w = (const T*)p.norm.k_weight;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        to_floats<T, 8>(raw[r][0], x[r][0]);
-        to_floats<T, 8>(raw[r][1], x[r][1]);
-        if (NORM && !is_v) norm_head<T, 8>(x[r][0], x[r][1], 3, D, p.norm.eps, p.norm.k_weight ? &w0 : nullptr, p.norm.k_weight ? &w1 : nullptr);
-    }
-    if (!is_v) {
-        // every angle of a token serves one pair of this head, so the lanes take them straight from the table
+                for (int i = 0; i < 8; ++i) {
+                    x[0][i] *= inv * (w ? to_float(w[c0 + i]) : 1.f);
+                    x[1][i] *= inv * (w ? to_float(w[c0 + half + i]) : 1.f);
+                }
+            }
+            // every angle of a token serves one pair of this head, so the lanes take them straight from the table
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const double omega = a.table ? 0.0 : rope_omega(c0 + i, D, a.log2_theta);
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                if (!is_new[r]) continue;
-                const int pos = p0 + slot0 + 32 * r;
-                const double2 cs = a.table ? a.table[(long)(pos - a.table_first) * half + c0 + i] : rope_cos_sin_at(pos, omega);
-                const float c = (float)cs.x, s = (float)cs.y, u = x[r][0][i], v = x[r][1][i];
-                x[r][0][i] = fmaf(u, c, -(v * s));
-                x[r][1][i] = fmaf(v, c, u * s);
+            for (int i = 0; i < 8; ++i) {
+                const double2 cs = a.table ? a.table[(long)(pos - a.table_first) * half + c0 + i] : rope_cos_sin(pos, c0 + i, D, a.log2_theta);
+                const float c = (float)cs.x, s = (float)cs.y, u = x[0][i], v = x[1][i];
+                x[0][i] = fmaf(u, c, -(v * s));
+                x[1][i] = fmaf(v, c, u * s);
             }
         }
-    }
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        if (is_new[r]) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) most = fmaxf(most, fmaxf(finite_abs(x[r][0][i]), finite_abs(x[r][1][i])));
-        }
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, fmaxf(finite_abs(x[0][i]), finite_abs(x[1][i])));
     }
 #pragma unroll
     for (int s = 16; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
     if ((threadIdx.x & 31) == 0) s_most[threadIdx.x >> 5] = most;
     __syncthreads();
+    most = s_most[threadIdx.x & (kAppend8Threads / 32 - 1)];
 #pragma unroll
-    for (int w = 0; w < kAppend8Threads / 32; ++w) most = fmaxf(most, s_most[w]);
-    const int e = scale_exponent8(most);
-    const float need = exp2_int(e), scale = held && old_scale > need ? old_scale : need;
+    for (int s = kAppend8Threads / 64; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
+    const float need = exp2_int(scale_exponent8(most)), scale = held && old_scale > need ? old_scale : need;
     const bool grew = held && scale > old_scale;
-    const float inv = 1.f / scale, again = grew ? old_scale * inv : 1.f;   // powers of two: exact
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        uint2* to_lo = reinterpret_cast<uint2*>(pool + (slot0 + 32 * r) * D + c0);
-        uint2* to_hi = reinterpret_cast<uint2*>(pool + (slot0 + 32 * r) * D + c0 + half);
-        if (is_new[r]) {
-            *to_lo = codes8(x[r][0], inv);
-            *to_hi = codes8(x[r][1], inv);
-        } else if (is_old[r]) {
-            if (grew) {
-                float y[8];
-                floats4(old[r][0].x, y); floats4(old[r][0].y, y + 4);
-                *to_lo = codes8(y, again);
-                floats4(old[r][1].x, y); floats4(old[r][1].y, y + 4);
-                *to_hi = codes8(y, again);
-            }
-        } else if (is_v) {
-            *to_lo = *to_hi = make_uint2(0u, 0u);          // behind the last token: nothing that could be NaN
-        }
+    const float down = 1.f / scale;                        // powers of two: exact
+    if (is_old && grew) {
+        const float again = old_scale * down;
+        floats4(r0.x, x[0]); floats4(r0.y, x[0] + 4);
+        floats4(r0.z, x[1]); floats4(r0.w, x[1] + 4);
+        *reinterpret_cast<uint2*>(at) = codes8(x[0], again);
+        *reinterpret_cast<uint2*>(at + half) = codes8(x[1], again);
+    } else if (is_new) {
+        *reinterpret_cast<uint2*>(at) = codes8(x[0], down);
+        *reinterpret_cast<uint2*>(at + half) = codes8(x[1], down);
+    } else if (is_v && !is_old) {
+        *reinterpret_cast<uint2*>(at) = *reinterpret_cast<uint2*>(at + half) = make_uint2(0u, 0u);      // behind the last token: nothing that could be NaN
     }
     if (threadIdx.x == 0 && (!held || grew)) *scale_at = scale;
 }

@@ -42,6 +42,27 @@ cudaError_t prepare_cache_kernels()
 
 namespace {
 
+// As launch_pdl, in clusters of `cluster` blocks along y.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_cluster_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st, Args&&... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 1;
+    attr[1].val.clusterDim.y = (unsigned)cluster;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
 evlnStatus_t launched(evlnHandle_t h, cudaError_t e)
 {
     return e == cudaSuccess ? EVLN_OK : cuda_fail(h, e);
@@ -270,13 +291,13 @@ evlnStatus_t evlnPaged8RopeAppend(evlnHandle_t h, const evlnPagedParams* p, cons
         const int L = h_cache_lens[b], n = h_new_offsets[b + 1] - h_new_offsets[b];
         if (n > 0) pages += ((long)L + n + kPage8 - 1) / kPage8 - L / kPage8;
     }
-    // queries: a block per 256 work items of a token where there are few tokens, else one per token
-    a.q_parts = total <= kRopeFewTokens ? ceil_div(a.r.Hq << a.r.vph_shift, kAppend8Threads) : 1;
-    const long blocks = 2 * pages * p->num_kv_heads + (long)total * a.q_parts;
+    a.q_threads = (a.r.Hq * 8 + 31) / 32 * 32;
+    if (a.q_threads > kAppend8Threads) a.q_threads = kAppend8Threads;
+    a.q_tokens = kAppend8Threads / a.q_threads;
+    const long blocks = 2 * pages * p->num_kv_heads + ((long)total + a.q_tokens - 1) / a.q_tokens;
     if (blocks > 0x3fffffffL) return EVLN_NOT_SUPPORTED;
     a.page_blocks = (int)(pages * p->num_kv_heads);
     a.div_hkv = make_fast_div((uint32_t)p->num_kv_heads);
-    a.div_parts = make_fast_div((uint32_t)a.q_parts);
     return launched(h, norm ? launch_pdl(append8_kernel<true>, dim3((unsigned)blocks), dim3(kAppend8Threads), 0, (cudaStream_t)stream, a, bl)
                             : launch_pdl(append8_kernel<false>, dim3((unsigned)blocks), dim3(kAppend8Threads), 0, (cudaStream_t)stream, a, bl));
 }
@@ -409,21 +430,11 @@ evlnStatus_t evlnKeyWeights(evlnHandle_t h, const evlnStepParams* p, const void*
     // few tiles: a cluster of CTAs for each, as many as the SMs (fp32: four blocks an SM) and the chunks allow
     int cluster = 1;
     while (cluster < kKwMaxCluster && 2 * cluster <= a.chunks && 2L * cluster * a.items <= (f32 ? 4L : 1L) * h->num_sms) cluster *= 2;
-    const bool whole = cluster > 1 || f32;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(whole || a.items < h->num_sms ? a.items : h->num_sms), (unsigned)cluster);
-    cfg.blockDim = dim3(f32 ? kKwF32Keys : kKwThreads);
-    cfg.stream = (cudaStream_t)stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = 1;
-    attr[1].val.clusterDim.y = (unsigned)cluster;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
-    if (f32) return launched(h, D == 128 ? cudaLaunchKernelEx(&cfg, key_weights_f32_kernel<128>, a) : cudaLaunchKernelEx(&cfg, key_weights_f32_kernel<64>, a));
+    const dim3 grid((unsigned)(cluster > 1 || f32 || a.items < h->num_sms ? a.items : h->num_sms), (unsigned)cluster);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (f32)
+        return launched(h, D == 128 ? launch_cluster_pdl(key_weights_f32_kernel<128>, grid, dim3(kKwF32Keys), 0, cluster, st, a)
+                                    : launch_cluster_pdl(key_weights_f32_kernel<64>, grid, dim3(kKwF32Keys), 0, cluster, st, a));
     CUtensorMap tm_k, tm_q;
     const cuuint64_t kdims[3] = {(cuuint64_t)D, (cuuint64_t)p->cache_capacity, (cuuint64_t)p->num_kv_heads};
     const cuuint64_t kstrides[2] = {(cuuint64_t)D * 2, (cuuint64_t)p->cache_capacity * D * 2};
@@ -432,8 +443,8 @@ evlnStatus_t evlnKeyWeights(evlnHandle_t h, const evlnStepParams* p, const void*
     const cuuint32_t kbox[3] = {64, kTileN, 1}, qbox[3] = {64, (cuuint32_t)a.chunk_rows, 1};
     if (!encode_map(h, &tm_k, k_cache, 3, kdims, kstrides, kbox)) return EVLN_INVALID_VALUE;
     if (!encode_map(h, &tm_q, q_rot, 3, qdims, qstrides, qbox)) return EVLN_INVALID_VALUE;
-    cfg.dynamicSmemBytes = D == 128 ? KeyWeightPlan<128>::kBytes : KeyWeightPlan<64>::kBytes;
-    return launched(h, D == 128 ? cudaLaunchKernelEx(&cfg, key_weights_kernel<128>, tm_k, tm_q, a) : cudaLaunchKernelEx(&cfg, key_weights_kernel<64>, tm_k, tm_q, a));
+    return launched(h, D == 128 ? launch_cluster_pdl(key_weights_kernel<128>, grid, dim3(kKwThreads), KeyWeightPlan<128>::kBytes, cluster, st, tm_k, tm_q, a)
+                                : launch_cluster_pdl(key_weights_kernel<64>, grid, dim3(kKwThreads), KeyWeightPlan<64>::kBytes, cluster, st, tm_k, tm_q, a));
 }
 
 evlnStatus_t evlnSelectKeys(evlnHandle_t h, const evlnGatherParams* p, const float* weights, int num_keys, int budget, int sinks, int recent,
@@ -441,6 +452,7 @@ evlnStatus_t evlnSelectKeys(evlnHandle_t h, const evlnGatherParams* p, const flo
 {
     evlnStatus_t s = check_gather_params(h, p);
     if (s != EVLN_OK) return s;
+    if (num_keys > (1 << 30)) return EVLN_NOT_SUPPORTED;
     if (num_keys < 0 || num_keys > p->store_capacity || budget < 0 || sinks < 0 || recent < 0 || (long)sinks + recent > budget) return EVLN_INVALID_VALUE;
     SelectArgs a = {};
     a.num_kept = budget < num_keys ? budget : num_keys;
@@ -450,8 +462,11 @@ evlnStatus_t evlnSelectKeys(evlnHandle_t h, const evlnGatherParams* p, const flo
     a.stride = p->store_capacity; a.num_keys = num_keys;
     a.sinks = sinks; a.recent = recent; a.open = budget - sinks - recent;
     if (a.num_kept == num_keys) a.sinks = a.recent = a.open = 0;
-    a.cached = num_keys <= kSelectCache;
-    return launched(h, launch_pdl(select_keys_kernel, dim3((unsigned)p->num_kv_heads), dim3(kSelectThreads), a.cached ? (size_t)num_keys * 4 : 0, (cudaStream_t)stream, a));
+    const int cluster = num_keys > kSelectSlice ? kSelectCluster : 1;
+    a.slice = ceil_div(num_keys, cluster);
+    a.cached = a.slice <= kSelectCache;
+    return launched(h, launch_cluster_pdl(select_keys_kernel, dim3((unsigned)p->num_kv_heads, (unsigned)cluster), dim3(kSelectThreads), a.cached ? (size_t)a.slice * 4 : 0,
+                                          cluster, (cudaStream_t)stream, a));
 }
 
 evlnStatus_t evlnGatherKeys(evlnHandle_t h, const evlnGatherParams* p, int num_kept, const int* kept, const float* weights, const void* k_store,
@@ -478,7 +493,7 @@ evlnStatus_t evlnGatherKeys(evlnHandle_t h, const evlnGatherParams* p, int num_k
     a.kept = kept;
     a.Hkv = p->num_kv_heads; a.D = p->head_dim; a.src_cap = p->store_capacity; a.dst_cap = p->work_capacity;
     a.num_kept = num_kept; a.rotate = rotate != 0;
-    a.log2_theta = log2(p->rope_theta);
+    for (int b = 0; b < 6; ++b) a.omega[b] = b == 0 ? exp2(-2.0 / a.D * log2(p->rope_theta)) : a.omega[b - 1] * a.omega[b - 1];
     a.table = (const double2*)p->rope_table;
     a.table_first = p->rope_table_first_pos;
     const int vec = 16 / elem_bytes(p->dtype);

@@ -1,9 +1,12 @@
 // Eviction: which keys of a kv head to keep, by weight, and the chosen ones laid out anew.
 //
-// select_keys_kernel: a block per kv head.  The threshold is the m-th largest of the weights in the open range, found digit by
-// digit (11, 11 and 10 bits of the float as an ordered integer, a histogram in shared memory each); then one ordered pass
-// writes the slots above it, of those equal to it the lowest, and the protected ends.  A thread holds a run of neighbouring slots, so one
-// scan over the block's counts gives every slot its place, ascending.
+// select_keys_kernel: a cluster of blocks per kv head, each with a run of its slots (one block where they are few).  The threshold is the m-th
+// largest of the weights in the open range, found digit by digit (11, 11 and 10 bits of the float as an ordered integer): each block
+// counts its keys' digits in shared memory, and the blocks read one another's counts over distributed shared memory, first 64 sums of 32 digits, then the
+// 32 digits in question.  Then one ordered pass writes the slots above the threshold, of those equal to it the lowest, and the protected ends,
+// ascending: scans over counts give every slot its place.
+// Bound: latency, and the instructions that a block has to fetch and issue, each a few times only; so loops stay rolled.  (20656 keys: one block per head
+// 15 us, 21 with its keys in registers and everything unrolled; eight blocks that read all 2048 counts of all, 13.)
 // gather_keys_kernel: a block takes a few working slots for all kv heads: their angles once into shared memory, then every
 // head's chosen key (turned as in rope_append.cuh, or copied) and value.
 #pragma once
@@ -19,10 +22,13 @@ struct SelectArgs {
     int* kept;               // [Hkv, num_kept]
     int stride, num_keys, num_kept;
     int sinks, recent, open; // open: how many of the slots between the ends are kept
-    int cached;              // the weights fit the block's shared memory
+    int slice;               // slots of a block
+    int cached;              // a slice fits the block's shared memory
 };
 
-constexpr int kSelectThreads = 1024, kSelectBins = 2048, kSelectCache = 48 * 1024;   // floats held on chip
+constexpr int kSelectThreads = 512, kSelectBins = 2048, kSelectCluster = 8, kSelectGroups = 64;      // groups of 32 digits
+constexpr int kSelectSlice = 4096;                        // most slots that one block takes alone
+constexpr int kSelectCache = 40 * 1024;                   // most slots of a slice held in shared memory
 
 // floats in order as unsigned integers; -0 as 0, NaN as -infinity
 __device__ __forceinline__ uint32_t ordered(float x)
@@ -31,96 +37,166 @@ __device__ __forceinline__ uint32_t ordered(float x)
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
-// Inclusive sums of a pair of counts over the block (all threads), by thread number.
-__device__ __forceinline__ int2 block_scan(int2 v, int2* s_warp)
+// Inclusive sums over the lanes of a warp.
+__device__ __forceinline__ int warp_scan(int x)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, v.x, o), y = __shfl_up_sync(0xffffffffu, v.y, o);
-        if (lane >= o) { v.x += x; v.y += y; }
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if ((int)(threadIdx.x & 31) >= o) x += y;
     }
-    if (lane == 31) s_warp[warp] = v;
-    __syncthreads();
-    if (warp == 0) {
-        int2 w = s_warp[lane];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, w.x, o), y = __shfl_up_sync(0xffffffffu, w.y, o);
-            if (lane >= o) { w.x += x; w.y += y; }
-        }
-        s_warp[lane] = w;
-    }
-    __syncthreads();
-    if (warp > 0) { v.x += s_warp[warp - 1].x; v.y += s_warp[warp - 1].y; }
-    return v;
+    return x;
 }
 
+// The cluster's blocks meet; what any of their threads wrote to shared memory before is visible to all after it (one warp's cluster-wide release
+// covers what the block's own meeting ordered before it).
+__device__ __forceinline__ void cluster_meet()
+{
+    __syncthreads();
+    if (threadIdx.x < 32) ptx::cluster_arrive();
+    else ptx::cluster_arrive_relaxed();
+    ptx::cluster_wait();
+}
+__device__ __forceinline__ int ld_cluster_int(const int* shared, int rank)
+{
+    return __float_as_int(ptx::ld_cluster_f32(ptx::map_to_cta(ptx::smem_u32(shared), rank)));
+}
+
+// grid (kv heads, cluster): blockIdx.y is the block's rank in its cluster.
 __global__ void __launch_bounds__(kSelectThreads, 1)
 select_keys_kernel(const SelectArgs a)
 {
-    extern __shared__ uint32_t s_key[];                   // [num_keys] where they fit
-    __shared__ int s_bin[kSelectBins];
-    __shared__ int2 s_warp[32];
-    __shared__ int s_digit, s_left;
-    const int g = blockIdx.x, tid = threadIdx.x;
+    extern __shared__ uint32_t s_key[];                   // [slice] where it fits
+    __shared__ __align__(16) int s_bin[3][kSelectBins];
+    __shared__ int s_group[3][kSelectGroups], s_sum[kSelectGroups];
+    __shared__ int s_found[3][2];
+    __shared__ int s_sure[kSelectThreads / 32], s_same[kSelectThreads / 32], s_total[2];
+    const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, csize = gridDim.y, rank = blockIdx.y;
     const float* w = a.weights + (long)g * a.stride;
     const int lo = a.sinks, hi = a.num_keys - a.recent;   // the open range
+    const int first = min(a.num_keys, rank * a.slice), last = min(a.num_keys, first + a.slice);      // this block's slots
+    for (int i = tid; i < 3 * kSelectBins / 4; i += kSelectThreads) reinterpret_cast<int4*>(s_bin)[i] = make_int4(0, 0, 0, 0);
+    __syncthreads();
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-    auto key = [&](int j) -> uint32_t { return a.cached ? s_key[j] : ordered(w[j]); };
-    if (a.cached)
-        for (int j = tid; j < a.num_keys; j += kSelectThreads) s_key[j] = ordered(w[j]);
-    uint32_t prefix = 0, mask = 0;
+    const bool search = a.num_kept < a.num_keys && a.open > 0, all = a.num_kept == a.num_keys;
+    const int from = max(lo, first), to = min(hi, last);  // of them open
+    uint32_t prefix = 0;
     int left = a.open;                                    // still to be found among the keys with this prefix
-    if (a.num_kept < a.num_keys && a.open > 0) {
+    if (search) {
+        // the keys, and their first digits: four loads in flight
+        constexpr int kBatch = 4;
+        for (int base = from + tid; base < to; base += kBatch * kSelectThreads) {
+            float x[kBatch];
 #pragma unroll
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-            for (int i = tid; i < kSelectBins; i += kSelectThreads) s_bin[i] = 0;
-            __syncthreads();
-            for (int j = lo + tid; j < hi; j += kSelectThreads) {
-                const uint32_t k = key(j);
-                if ((k & mask) == prefix) atomicAdd(&s_bin[(k >> shift) & ((1 << bits) - 1)], 1);
+            for (int i = 0; i < kBatch; ++i) x[i] = base + i * kSelectThreads < to ? w[base + i * kSelectThreads] : 0.f;
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int j = base + i * kSelectThreads;
+                if (j >= to) break;
+                const uint32_t k = ordered(x[i]);
+                if (a.cached) s_key[j - first] = k;
+                atomicAdd(&s_bin[0][k >> 21], 1);
             }
-            __syncthreads();
-            // bins from the largest digit down, two a thread: where does the count reach `left`?
-            const int d0 = kSelectBins - 1 - 2 * tid, n0 = s_bin[d0], n1 = s_bin[d0 - 1];
-            const int upto = block_scan(make_int2(n0 + n1, 0), s_warp).x, before = upto - n0 - n1;
-            if (before < left && upto >= left) {
-                const bool second = before + n0 < left;
-                s_digit = second ? d0 - 1 : d0;
-                s_left = left - before - (second ? n0 : 0);
-            }
-            __syncthreads();
-            prefix |= (uint32_t)s_digit << shift;
-            mask |= ((1u << bits) - 1u) << shift;
-            left = s_left;
-            __syncthreads();
         }
     }
-    __syncthreads();
-    // ---- every thread a run of neighbouring slots (of odd length: the runs start in different banks) ----
-    const bool all = a.num_kept == a.num_keys;
-    const int run = ((a.num_keys + kSelectThreads - 1) / kSelectThreads) | 1, j0 = min(a.num_keys, tid * run), j1 = min(a.num_keys, j0 + run);
-    int2 n = make_int2(0, 0);                             // kept for certain, equal to the threshold
-    for (int j = j0; j < j1; ++j) {
-        const uint32_t k = key(j);
-        const bool end = j < lo || j >= hi || all;
-        n.x += end || (a.open > 0 && k > prefix);
-        n.y += !end && a.open > 0 && k == prefix;
+    auto key = [&](int j) -> uint32_t { return a.cached ? s_key[j - first] : ordered(w[j]); };
+    for (int pass = 0; search && pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 1 ? 21 : 10;
+        if (pass > 0) {
+            for (int j = from + tid; j < to; j += kSelectThreads) {
+                const uint32_t k = key(j);
+                if (k >> above == prefix >> above) atomicAdd(&s_bin[pass][(k >> shift) & (pass == 2 ? 1023 : 2047)], 1);
+            }
+        }
+        __syncthreads();
+        {   // sums of 32 digits, eight lanes of four each
+            const int4 n = *reinterpret_cast<const int4*>(&s_bin[pass][4 * tid]);
+            int sum = n.x + n.y + n.z + n.w;
+            for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if ((lane & 7) == 0) s_group[pass][tid >> 3] = sum;
+        }
+        if (csize > 1) {
+            cluster_meet();
+            int sum = ld_cluster_int(&s_group[pass][tid >> 3], tid & 7);
+            for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if ((lane & 7) == 0) s_sum[tid >> 3] = sum;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            // the group in which the count from the largest digit down reaches `left` (lane: two groups), then the digit
+            const int* sums = csize > 1 ? s_sum : s_group[pass];
+            const int g0 = kSelectGroups - 1 - 2 * lane, n0 = sums[g0], n1 = sums[g0 - 1], upto = warp_scan(n0 + n1);
+            const int who = __ffs(__ballot_sync(0xffffffffu, upto >= left)) - 1;
+            int group = g0, before = upto - n0 - n1;
+            if (before + n0 < left) { --group; before += n0; }
+            group = __shfl_sync(0xffffffffu, group, who);
+            before = __shfl_sync(0xffffffffu, before, who);
+            const int digit = 32 * group + 31 - lane;
+            int n = 0;
+            if (csize > 1) {
+#pragma unroll
+                for (int r = 0; r < kSelectCluster; ++r) n += ld_cluster_int(&s_bin[pass][digit], r);
+            } else {
+                n = s_bin[pass][digit];
+            }
+            const int sum = warp_scan(n), at = __ffs(__ballot_sync(0xffffffffu, before + sum >= left)) - 1;
+            if (lane == at) {
+                s_found[pass][0] = digit;
+                s_found[pass][1] = left - before - (sum - n);
+            }
+        }
+        __syncthreads();
+        prefix |= (uint32_t)s_found[pass][0] << shift;
+        left = s_found[pass][1];
     }
-    int2 at = block_scan(n, s_warp);
-    at.x -= n.x;
-    at.y -= n.y;
+    // ---- places: every warp a run of neighbouring slots, 32 at a time ----
+    const int per = ((a.slice + kSelectThreads - 1) / kSelectThreads) * 32, j0 = min(last, first + warp * per), j1 = min(last, j0 + per);
+    int sure = 0, same = 0;                               // this warp's slots kept for certain, and equal to the threshold
+    for (int j = j0 + lane; j - lane < j1; j += 32) {
+        const bool open = j >= from && j < to, end = j < j1 && (!open || all);
+        const uint32_t k = open && search ? key(j) : 0u;
+        sure += __popc(__ballot_sync(0xffffffffu, end || (search && j < j1 && k > prefix)));
+        same += __popc(__ballot_sync(0xffffffffu, search && open && j < j1 && k == prefix));
+    }
+    if (lane == 0) {
+        s_sure[warp] = sure;
+        s_same[warp] = same;
+    }
+    __syncthreads();
+    sure = warp_scan(lane < kSelectThreads / 32 ? s_sure[lane] : 0);                     // (every warp for itself)
+    same = warp_scan(lane < kSelectThreads / 32 ? s_same[lane] : 0);
+    if (tid == 31) {
+        s_total[0] = sure;
+        s_total[1] = same;
+    }
+    sure = warp > 0 ? __shfl_sync(0xffffffffu, sure, warp - 1) : 0;                      // kept, and equal, before this warp's slots
+    same = warp > 0 ? __shfl_sync(0xffffffffu, same, warp - 1) : 0;
+    if (csize > 1) {
+        cluster_meet();
+        int x = lane < rank ? ld_cluster_int(&s_total[0], lane) : 0, y = lane < rank ? ld_cluster_int(&s_total[1], lane) : 0;
+        for (int o = 1; o < 8; o <<= 1) {
+            x += __shfl_xor_sync(0xffffffffu, x, o);
+            y += __shfl_xor_sync(0xffffffffu, y, o);
+        }
+        sure += __shfl_sync(0xffffffffu, x, 0);
+        same += __shfl_sync(0xffffffffu, y, 0);
+    }
     int* out = a.kept + (long)g * a.num_kept;
-    for (int j = j0; j < j1; ++j) {
-        const uint32_t k = key(j);
-        const bool end = j < lo || j >= hi || all;
-        const bool sure = end || (a.open > 0 && k > prefix), equal = !end && a.open > 0 && k == prefix;
-        if (sure || (equal && at.y < left)) out[at.x + min(at.y, left)] = j;
-        at.x += sure;
-        at.y += equal;
+    const unsigned below = (1u << lane) - 1u;
+    for (int j = j0 + lane; j - lane < j1; j += 32) {
+        const bool open = j >= from && j < to, end = j < j1 && (!open || all);
+        const uint32_t k = open && search ? key(j) : 0u;
+        const bool mine = end || (search && j < j1 && k > prefix), equal = search && open && j < j1 && k == prefix;
+        const unsigned s = __ballot_sync(0xffffffffu, mine), e = __ballot_sync(0xffffffffu, equal);
+        const int turn = same + __popc(e & below);
+        if (mine || (equal && turn < left)) out[sure + __popc(s & below) + min(turn, left)] = j;
+        sure += __popc(s);
+        same += __popc(e);
+    }
+    if (csize > 1) {
+        ptx::cluster_arrive_relaxed();                    // nobody leaves while another block may read its counts
+        ptx::cluster_wait();
     }
 }
 
@@ -133,7 +209,7 @@ struct GatherKeysArgs {
     float* w_dst;            // [Hkv, dst_cap]
     const int* kept;         // [Hkv, num_kept]
     int Hkv, D, src_cap, dst_cap, num_kept, rotate;
-    double log2_theta;
+    double omega[6];         // theta^(-2 2^b / D): a frequency is a product of them
     const double2* table;    // optional
     int table_first;
     int vph_shift;           // log2 of the 16-byte vectors per half head vector
@@ -141,46 +217,61 @@ struct GatherKeysArgs {
 
 constexpr int kGatherKeysThreads = 256;
 template <typename T>
-__global__ void __launch_bounds__(kGatherKeysThreads)
+__global__ void __launch_bounds__(kGatherKeysThreads, 5)
 gather_keys_kernel(const GatherKeysArgs a)
 {
     constexpr int V = VecTraits<T>::kVec;
     __shared__ __align__(16) typename Rotation<T>::Angle s_angle[8][Rotation<T>::kAngles];
-    const int D = a.D, half = D / 2, tid = threadIdx.x;
-    const int slots = kGatherKeysThreads / half;          // 4 or 8 working slots a block
-    const int p0 = blockIdx.x * slots, here = min(slots, a.num_kept - p0);
-    const int vph = a.vph_shift, k_items = 1 << vph, per_head = 3 << vph;      // pairs of a key, vectors of a value
-    const double omega = a.rotate && !a.table ? rope_omega(tid % half, D, a.log2_theta) : 0.0;
+    const int D = a.D, half = D / 2, tid = threadIdx.x, vph = a.vph_shift;
+    const int log_slots = D == 128 ? 2 : 3;               // 4 or 8 working slots a block
+    const int p0 = blockIdx.x << log_slots, j = tid & (half - 1), angle_slot = tid >> (D == 128 ? 6 : 5);
+    // theta^(-2 j / D) as a product of at most six powers.  (Without a table a block is bound by arithmetic in double precision: a sine and
+    // cosine, 80 instructions, an exponential 70 more, 4.4 us of 9 for 4096 slots of 4 heads.)
+    double omega = 1.0;
+    if (a.rotate && !a.table) {
+#pragma unroll
+        for (int b = 0; b < 6; ++b)
+            if ((j >> b) & 1) omega *= a.omega[b];
+    }
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
+    // A work item: a pair of 16-byte vectors (channels e V .., + D/2) of a slot's key or value of one head; a key's lanes, then a value's.
+    const int items = a.Hkv << (log_slots + vph + 1);
+    long dst = 0;
+    uint4 x0, x1;
+    bool there = false;
+    auto load = [&](int it) {
+        const int row = it >> (vph + 1), e = it & ((1 << vph) - 1), p = p0 + (row & ((1 << log_slots) - 1)), g = row >> log_slots;
+        there = it < items && p < a.num_kept;
+        if (!there) return;
+        const int from = a.kept[(long)g * a.num_kept + p];
+        const bool good = (unsigned)from < (unsigned)a.src_cap, is_v = (it >> vph) & 1;
+        dst = ((long)g * a.dst_cap + p) * D + e * V;
+        x0 = x1 = make_uint4(0u, 0u, 0u, 0u);
+        if (good) {
+            const T* src = (const T*)(is_v ? a.v_src : a.k_src) + ((long)g * a.src_cap + from) * D + e * V;
+            x0 = *reinterpret_cast<const uint4*>(src);
+            x1 = *reinterpret_cast<const uint4*>(src + half);
+        }
+        if (e == 0 && is_v && a.w_src) a.w_dst[(long)g * a.dst_cap + p] = good ? a.w_src[(long)g * a.src_cap + from] : 0.f;
+    };
+    load(tid);                                            // in flight while the angles are formed
     if (a.rotate) {
-        const int p = p0 + tid / half, j = tid % half;
-        if (tid / half < here) Rotation<T>::put(s_angle[tid / half], j, a.table ? a.table[(long)(p - a.table_first) * half + j] : rope_cos_sin_at(p, omega));
+        const int p = p0 + angle_slot;
+        if (p < a.num_kept) Rotation<T>::put(s_angle[angle_slot], j, a.table ? a.table[(long)(p - a.table_first) * half + j] : rope_cos_sin_at(p, omega));
         __syncthreads();
     }
-    const int items = here * a.Hkv * per_head;
-    for (int it = tid; it < items; it += kGatherKeysThreads) {
-        const int row = it / per_head, e = it - row * per_head;                // row: slot and head, slots side by side
-        const int g = row / here, s = row - g * here, p = p0 + s;
-        const int from = a.kept[(long)g * a.num_kept + p];
-        const bool good = (unsigned)from < (unsigned)a.src_cap;
-        const long src = ((long)g * a.src_cap + (good ? from : 0)) * D, dst = ((long)g * a.dst_cap + p) * D;
-        const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-        if (e < k_items) {
-            const T* k = (const T*)a.k_src + src + e * V;
-            uint4 lo = good ? *reinterpret_cast<const uint4*>(k) : none, hi = good ? *reinterpret_cast<const uint4*>(k + half) : none;
-            if (a.rotate) {
-                uint4 x = lo, y = hi;
-                Rotation<T>::turn(s_angle[s], e, x, y, lo, hi);
-            }
-            T* to = (T*)a.k_dst + dst + e * V;
-            *reinterpret_cast<uint4*>(to) = lo;
-            *reinterpret_cast<uint4*>(to + half) = hi;
-            if (e == 0 && a.w_src) a.w_dst[(long)g * a.dst_cap + p] = good ? a.w_src[(long)g * a.src_cap + from] : 0.f;
-        } else {
-            const int d = (e - k_items) * V;
-            *reinterpret_cast<uint4*>((T*)a.v_dst + dst + d) = good ? *reinterpret_cast<const uint4*>((const T*)a.v_src + src + d) : none;
+    for (int it = tid; it < items;) {
+        if (there) {
+            const bool is_v = (it >> vph) & 1;
+            uint4 y0 = x0, y1 = x1;
+            if (a.rotate && !is_v) Rotation<T>::turn(s_angle[(it >> (vph + 1)) & ((1 << log_slots) - 1)], it & ((1 << vph) - 1), x0, x1, y0, y1);
+            T* to = (T*)(is_v ? a.v_dst : a.k_dst) + dst;
+            *reinterpret_cast<uint4*>(to) = y0;
+            *reinterpret_cast<uint4*>(to + half) = y1;
         }
+        it += kGatherKeysThreads;
+        if (it < items) load(it);
     }
 }
 
