@@ -1,4 +1,4 @@
-// Step attention over a paged cache in 8 bits (cache8.cuh), for up to a few hundred query rows per kv head.
+// Step attention over a paged cache in 8 bits (cache8.cuh), for up to 64 query rows per kv head and episode.
 //
 //     out = softmax(scale * q K^T) V,    K, V = code * scale of its page,    a query sees the keys up to its own position
 //
@@ -17,7 +17,7 @@
 //
 // A block: RG row groups x KG key groups of warps, each warp 8 NQ rows.  A key group takes a RUN of neighbouring stages (32 keys:
 // 4 KB keys + 4 KB values, TMA, 128-byte swizzle) through a ring of its own, which one warp of it refills as it goes, and walks it
-// unit by unit (unit: episode, kv head, tile of rows).  Nothing is shared between key groups until all are done: then the
+// unit by unit (unit: episode, kv head).  Nothing is shared between key groups until all are done: then the
 // results of neighbouring runs that ended in the same unit are joined in the shared memory that the rings leave.  (Stages dealt
 // to the warps in turn, which joins all of them at the end of every unit, took 45 us for 16 ragged episodes of a token, runs 38.)
 // Runs are equally long, KG of them per SM; a unit that the runs cut across blocks leaves normalised parts, which merge8_kernel
@@ -41,25 +41,25 @@ constexpr float kA8LeastRatio = -40.f;                // log2 of the smallest va
 
 template <int NQ, int RG>
 struct Attn8Plan {
-    // up to 16 rows: twelve warps of 168 registers (three a scheduler hide each other's chains); 32: eight of 255
-    static constexpr int kWarps = NQ <= 2 ? 12 : 8, kThreads = 32 * kWarps;
-    // (8 rows need no more than 144, which leaves the SM room for blocks of the merge kernel)
-    static constexpr int kRegs = NQ == 1 ? 144 : NQ == 2 ? 168 : 255;
+    // Twelve warps, three a scheduler that hide each other's chains.  (Eight of 255 registers with 32 rows each take 5 to 10 % less for large batches of
+    // 17 to 64 rows, 16 episodes of 8000 keys 86 us and 95, but more where latency counts, one of 4096 keys 14.5 and 12.5.)
+    static constexpr int kWarps = 12, kThreads = 32 * kWarps;
+    // (8 rows need no more than 144 registers, which leaves the SM room for blocks of the merge kernel)
+    static constexpr int kRegs = NQ == 1 ? 144 : 168;
     static constexpr int kWarpRows = 8 * NQ, kRows = kWarpRows * RG;
     static constexpr int kKeyGroups = kWarps / RG;
-    static constexpr bool kQRegs = NQ <= 2;                                     // queries in registers, or in shared memory in operand order
-    static constexpr int kQBytes = kQRegs ? 0 : kWarps * (NQ / 2) * 8 * 512;
     static constexpr int kStatBytes = kWarps * kWarpRows * 8 + 64;             // references and sums, the units that the runs ended in
     static constexpr int kBarBytes = 512;
-    static constexpr int kRest = kQBytes + kStatBytes + kBarBytes + 1024;
+    static constexpr int kRest = kStatBytes + kBarBytes + 1024;
     static constexpr int kFit = (227 * 1024 - kRest) / kA8StageBytes / kKeyGroups;
     static constexpr int kSlots = kFit < 32 ? kFit : 32;
     static constexpr int kRing = kKeyGroups * kSlots * kA8StageBytes;
-    static constexpr int kQOff = kRing, kStatOff = kQOff + kQBytes, kBarOff = kStatOff + kStatBytes;
+    static constexpr int kStatOff = kRing, kBarOff = kStatOff + kStatBytes;
     static constexpr int kBytes = kRing + kRest;
     static_assert(kSlots >= 2, "a stage in flight beside the one that is read");
     static_assert(16 * kKeyGroups * kSlots + 8 <= kBarBytes, "barriers");
-    static_assert(kWarps * kWarpRows * kA8OStride * 4 <= kRing + kQBytes, "the joint's buffers");
+    static_assert(kWarps * kWarpRows * kA8OStride * 4 <= kRing, "the joint's buffers");
+    static_assert(NQ <= 2, "a 16-row tile of queries in a warp's registers");
     static_assert(kBarOff % 8 == 0 && kBytes <= 227 * 1024, "shared memory of a block");
 };
 
@@ -70,8 +70,8 @@ struct Attn8Args {
     const int* page_table;
     __nv_bfloat16* out;              // [tokens, Hq, 128]
     float* lse_out;                  // [tokens, Hq] or null
-    float* o_part;                   // [2 * runs, rows of a tile, 128]
-    float* lse_part;                 // [2 * runs, rows of a tile], log2
+    float* o_part;                   // [2 * runs, rows of a block, 128]
+    float* lse_part;                 // [2 * runs, rows of a block], log2
     int* status;
     int Hkv, G, rows, batch, max_pages;
     int run, total;                  // stages of a run, of the batch
@@ -79,13 +79,12 @@ struct Attn8Args {
     FastDiv div_g;
 };
 
-// Unit u of episode b: kv head u / tiles, row tile u % tiles.  lens.item_off[b]: stages before the episode.
+// A unit: a kv head of an episode.  lens.item_off[b]: stages before the episode.
 struct Unit8 {
-    int b, g, tile, L, n, stages;
+    int b, g, L, n, stages;
     int first;                       // the batch's stages before the unit
 };
-template <int ROWS>
-__device__ __forceinline__ Unit8 unit8_at(const BatchLens& lens, int batch, int Hkv, int G, int stage)
+__device__ __forceinline__ Unit8 unit8_at(const BatchLens& lens, int batch, int stage)
 {
     Unit8 u;
     int lo = 0, hi = batch;          // largest b with item_off[b] <= stage (episodes without new tokens have none)
@@ -97,11 +96,8 @@ __device__ __forceinline__ Unit8 unit8_at(const BatchLens& lens, int batch, int 
     u.L = lens.cache_len[lo];
     u.n = lens.new_off[lo + 1] - lens.new_off[lo];
     u.stages = (u.L + u.n + kA8Keys - 1) / kA8Keys;
-    const int at = (int)((unsigned)(stage - lens.item_off[lo]) / (unsigned)u.stages);
-    const int tiles = (u.n * G + ROWS - 1) / ROWS;
-    u.g = (int)((unsigned)at / (unsigned)tiles);
-    u.tile = at - u.g * tiles;
-    u.first = lens.item_off[lo] + at * u.stages;
+    u.g = (int)((unsigned)(stage - lens.item_off[lo]) / (unsigned)u.stages);
+    u.first = lens.item_off[lo] + u.g * u.stages;
     return u;
 }
 
@@ -131,7 +127,6 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
 {
     using Plan = Attn8Plan<NQ, RG>;
     constexpr int ROWS = Plan::kRows, KG = Plan::kKeyGroups, SLOTS = Plan::kSlots, WROWS = Plan::kWarpRows;
-    constexpr int MT = (NQ + 1) / 2, HN = NQ == 1 ? 1 : 2;              // 16-row tiles of the score products, 8-row halves of them in use
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
@@ -161,7 +156,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         }
     }
     Unit8 u = {};
-    if (mine > 0) u = unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, r0);
+    if (mine > 0) u = unit8_at(lens, a.batch, r0);
     __syncthreads();
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
@@ -173,7 +168,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         Ahead h = {0, 0.f, 0.f};
         if (i < mine) {
             Unit8 w = u;
-            if (r0 + i >= u.first + u.stages) w = unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, r0 + i);
+            if (r0 + i >= u.first + u.stages) w = unit8_at(lens, a.batch, r0 + i);
             const int key = (r0 + i - w.first) * kA8Keys;
             const int page = a.page_table[(long)w.b * a.max_pages + key / kPage8], at = page * a.Hkv + w.g;
             h.row = at * kPage8 + (key & (kPage8 - 1));
@@ -189,22 +184,21 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         ptx::tma_load_2d(dst + kA8StageBytes / 2, &tm_v, bar, 0, row);
     };
     // ---- a unit's queries: halves of each row's own size, in operand order (k-step c: channels 16 c + 4 quad .. + 3 of rows lrow, lrow + 8) ----
-    uint4* q_at = reinterpret_cast<uint4*>(smem_gen + Plan::kQOff + warp * (MT * 8 * 512)) + lane;
-    uint32_t qf[Plan::kQRegs ? 8 : 1][2 * HN];
-    float factor[MT][HN];
-    auto load_q = [&](int mt, uint2 (&raw)[HN][8]) {
+    uint32_t qf[8][2 * NQ];
+    float factor[NQ];
+    auto load_q = [&](uint2 (&raw)[NQ][8]) {
 #pragma unroll
-        for (int h = 0; h < HN; ++h) {
-            const int rl = u.tile * ROWS + rg * WROWS + mt * 16 + h * 8 + lrow;
+        for (int h = 0; h < NQ; ++h) {
+            const int rl = rg * WROWS + h * 8 + lrow;
             const uint2* src = reinterpret_cast<const uint2*>(a.q_rot + ((long)u.g * a.rows + (long)lens.new_off[u.b] * a.G + rl) * 128) + quad;
 #pragma unroll
             for (int c = 0; c < 8; ++c) raw[h][c] = rl < u.n * a.G ? src[4 * c] : make_uint2(0u, 0u);
         }
     };
-    auto put_q = [&](int mt, const uint2 (&raw)[HN][8]) {
-        float up[HN];
+    auto put_q = [&](const uint2 (&raw)[NQ][8]) {
+        float up[NQ];
 #pragma unroll
-        for (int h = 0; h < HN; ++h) {
+        for (int h = 0; h < NQ; ++h) {
             float most = 0.f;
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
@@ -216,21 +210,14 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             int e = 14 - ((int)(__float_as_uint(most) >> 23) - 127);                 // the row's maximum into [2^14, 2^15)
             e = e > 100 ? 100 : e;
             up[h] = exp2_int(e);
-            factor[mt][h] = a.scale_log2 * exp2_int(-e);
+            factor[h] = a.scale_log2 * exp2_int(-e);
         }
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
-            uint32_t f[2 * HN];                                                       // channels 4 quad, + 1 of each half, then + 2, + 3
 #pragma unroll
-            for (int h = 0; h < HN; ++h) {
-                f[h] = pack_f16x2(__uint_as_float(raw[h][c].x << 16) * up[h], __uint_as_float(raw[h][c].x & 0xffff0000u) * up[h]);
-                f[h + HN] = pack_f16x2(__uint_as_float(raw[h][c].y << 16) * up[h], __uint_as_float(raw[h][c].y & 0xffff0000u) * up[h]);
-            }
-            if constexpr (Plan::kQRegs) {
-#pragma unroll
-                for (int e = 0; e < 2 * HN; ++e) qf[c][e] = f[e];
-            } else {
-                q_at[(mt * 8 + c) * 32] = make_uint4(f[0], f[1], f[2], f[3]);         // (read by this lane only)
+            for (int h = 0; h < NQ; ++h) {                                            // channels 4 quad, + 1 of each half, then + 2, + 3
+                qf[c][h] = pack_f16x2(__uint_as_float(raw[h][c].x << 16) * up[h], __uint_as_float(raw[h][c].x & 0xffff0000u) * up[h]);
+                qf[c][h + NQ] = pack_f16x2(__uint_as_float(raw[h][c].y << 16) * up[h], __uint_as_float(raw[h][c].y & 0xffff0000u) * up[h]);
             }
         }
     };
@@ -238,20 +225,12 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     Ahead now, next;
     {
         // the first unit's queries are on their way while the first stages' pages are looked up
-        uint2 raw[HN][8];
-        if (mine > 0) load_q(0, raw);
+        uint2 raw[NQ][8];
+        if (mine > 0) load_q(raw);
         now = look(0);
         if (rg == 0 && lane < SLOTS && lane < mine) load(lane, now.row);
         __syncwarp();
-        if (mine > 0) put_q(0, raw);
-    }
-#pragma unroll
-    for (int mt = 1; mt < MT; ++mt) {
-        uint2 raw[HN][8];
-        if (mine > 0) {
-            load_q(mt, raw);
-            put_q(mt, raw);
-        }
+        if (mine > 0) put_q(raw);
     }
     next = look(1);
 
@@ -263,21 +242,18 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     bool left = false;                                 // the unit at hand goes to the joint
     while (i < mine) {
         if (i > 0) {
-            u = unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, r0 + i);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                uint2 raw[HN][8];
-                load_q(mt, raw);
-                put_q(mt, raw);
-            }
+            u = unit8_at(lens, a.batch, r0 + i);
+            uint2 raw[NQ][8];
+            load_q(raw);
+            put_q(raw);
         }
         const int begin = r0 + i, end = min(r1, u.first + u.stages);
-        const int rows_here = u.n * a.G - u.tile * ROWS, row0 = u.tile * ROWS + rg * WROWS;      // this warp's rows: row0 ..
+        const int rows_here = u.n * a.G, row0 = rg * WROWS;      // this warp's rows: row0 ..
         int last[NQ];                                  // the row's last key
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
             const int r = q * 8 + lrow;
-            last[q] = rg * WROWS + r < rows_here ? u.L + (int)fast_div((uint32_t)(row0 + r), a.div_g) : u.L + u.n - 1;
+            last[q] = row0 + r < rows_here ? u.L + (int)fast_div((uint32_t)(row0 + r), a.div_g) : u.L + u.n - 1;
 #pragma unroll
             for (int c = 0; c < 8; ++c) o[q][c][0] = o[q][c][1] = o[q][c][2] = o[q][c][3] = 0.f;
             m[q] = -INFINITY;
@@ -295,34 +271,23 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             const int key0 = (r0 + i - u.first) * kA8Keys;
             ok = ok && warp_wait(bar_full + 8 * slot, parity, kDevTimeoutMmaKV, a.status, s_abort, lane);
             if (ok) {
-                // ---- scores: 16 MT rows x 32 keys ----
-                float sc[MT][4][4];
+                // ---- scores: 16 rows (8 of them used, NQ = 1) x 32 keys ----
+                float sc[4][4];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) sc[mt][t][0] = sc[mt][t][1] = sc[mt][t][2] = sc[mt][t][3] = 0.f;
+                for (int t = 0; t < 4; ++t) sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
-                    uint32_t kk[4], f[MT][4];
+                    uint32_t kk[4], f[4];
                     ptx::ldmatrix_x4(kk, kbase ^ (c << 4));
-                    if constexpr (NQ == 1) {
-                        f[0][0] = qf[c][0]; f[0][2] = qf[c][1]; f[0][1] = f[0][3] = 0u;       // (no rows in the lower half)
-                    } else if constexpr (Plan::kQRegs) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) f[0][e] = qf[c][e];
-                    } else {
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-                            const uint4 x = q_at[(mt * 8 + c) * 32];
-                            f[mt][0] = x.x; f[mt][1] = x.y; f[mt][2] = x.z; f[mt][3] = x.w;
-                        }
-                    }
+                    f[0] = qf[c][0];
+                    f[2] = qf[c][NQ];
+                    f[1] = NQ == 2 ? qf[c][1] : 0u;
+                    f[3] = NQ == 2 ? qf[c][2 * NQ - 1] : 0u;
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
                         uint32_t b0, b1;
                         halves4(kk[t], b0, b1);
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) mma_f16(sc[mt][t], f[mt], b0, b1);
+                        mma_f16(sc[t], f, b0, b1);
                     }
                 }
                 // ---- softmax: references, probabilities, sums ----
@@ -337,18 +302,17 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                         for (int t = 0; t < 4; ++t)
 #pragma unroll
                             for (int e = 0; e < 2; ++e)
-                                if (key0 + 8 * t + 2 * quad + e > last[q]) sc[q >> 1][t][2 * (q & 1) + e] = -INFINITY;
+                                if (key0 + 8 * t + 2 * quad + e > last[q]) sc[t][2 * q + e] = -INFINITY;
                 }
                 uint32_t p[NQ][2][2];                                 // the transposed product's operand: two k-steps of 16 keys
                 bool moved = grew && shrink > 0.f;
                 float keep[NQ];
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
-                    const int mt = q >> 1, h = q & 1;
-                    const float f = factor[mt][h] * ks;               // > 0
+                    const float f = factor[q] * ks;                   // > 0
                     float top = -INFINITY;
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) top = ptx::max3(top, sc[mt][t][2 * h], sc[mt][t][2 * h + 1]);
+                    for (int t = 0; t < 4; ++t) top = ptx::max3(top, sc[t][2 * q], sc[t][2 * q + 1]);
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * f;
                     const bool move = top > m[q] + kA8Headroom;       // (from -inf: whenever there is a score)
@@ -363,7 +327,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
                         float x, y;
-                        ptx::unpack2(ptx::fma2(ptx::pack2(sc[mt][t][2 * h], sc[mt][t][2 * h + 1]), f2, off2), x, y);
+                        ptx::unpack2(ptx::fma2(ptx::pack2(sc[t][2 * q], sc[t][2 * q + 1]), f2, off2), x, y);
                         x = ptx::ex2(x);
                         y = ptx::ex2(y);
                         sum2 = ptx::add2(sum2, ptx::pack2(x, y));
@@ -430,14 +394,14 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                 for (int e = 0; e < 2; ++e) {
                     const float by = __shfl_sync(0xffffffffu, by_row, 8 * quad + 4 * e), lse2 = __shfl_sync(0xffffffffu, lse_row, 8 * quad + 4 * e);
                     const int r = q * 8 + 2 * quad + e;
-                    if (rg * WROWS + r >= rows_here) continue;
+                    if (row0 + r >= rows_here) continue;
                     if (whole) {
                         const long at = out_row8(a, lens, u, row0 + r);
 #pragma unroll
                         for (int c = 0; c < 8; ++c) reinterpret_cast<uint32_t*>(a.out + at * 128)[8 * c + lrow] = ptx::pack_bf16x2(o[q][c][e] * by, o[q][c][2 + e] * by);
                         if (a.lse_out && lrow == 0) a.lse_out[at] = lse2 * kLn2;
                     } else {
-                        const long at = 2L * run * ROWS + rg * WROWS + r;
+                        const long at = 2L * run * ROWS + row0 + r;
 #pragma unroll
                         for (int c = 0; c < 8; ++c) reinterpret_cast<float2*>(a.o_part + at * 128)[8 * c + lrow] = make_float2(o[q][c][e] * by, o[q][c][2 + e] * by);
                         if (lrow == 0) a.lse_part[at] = lse2;
@@ -496,10 +460,10 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         int k1 = k0 + 1;
         while (k1 < KG && s_unit[k1] == at_unit) ++k1;
         if (at_unit >= 0) {
-            const Unit8 w = left && u.first == at_unit ? u : unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, at_unit);
+            const Unit8 w = left && u.first == at_unit ? u : unit8_at(lens, a.batch, at_unit);
             const int first_run = blockIdx.x * KG + k0, ends = min(a.total, (blockIdx.x * KG + k1) * a.run);
             const bool whole = first_run * a.run <= w.first && ends == w.first + w.stages;
-            const int rows_here = min(ROWS, w.n * a.G - w.tile * ROWS);
+            const int rows_here = w.n * a.G;
             for (int r = tid >> 5; r < rows_here; r += Plan::kWarps) {               // a warp per row, four channels a lane
                 const int at0 = (k0 * RG + r / WROWS) * WROWS + r % WROWS;
                 float sum = 0.f;
@@ -515,7 +479,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                 const float by = sum == 0.f ? 0.f : 1.f / sum, lse2 = sum == 0.f ? -INFINITY : s_m[at0] + log2f(sum);
                 x.x *= by; x.y *= by; x.z *= by; x.w *= by;
                 if (whole) {
-                    const long at = out_row8(a, lens, w, w.tile * ROWS + r);
+                    const long at = out_row8(a, lens, w, r);
                     reinterpret_cast<uint2*>(a.out + at * 128)[lane] = make_uint2(ptx::pack_bf16x2(x.x, x.y), ptx::pack_bf16x2(x.z, x.w));
                     if (a.lse_out && lane == 0) a.lse_out[at] = lse2 * kLn2;
                 } else {
@@ -552,7 +516,7 @@ merge8_kernel(const Attn8Args a, const __grid_constant__ BatchLens lens, const _
     int u1, ra, rb;
     bool on;                                           // the unit's last run goes on behind it
     auto cut = [&](int first) -> bool {
-        u = unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, first);
+        u = unit8_at(lens, a.batch, first);
         u1 = u.first + u.stages;
         ra = u.first / a.run;
         rb = (u1 - 1) / a.run;
@@ -566,7 +530,7 @@ merge8_kernel(const Attn8Args a, const __grid_constant__ BatchLens lens, const _
     } else {
         next = blockIdx.x * KG * a.run;
         to = min(a.total, next + KG * a.run);
-        u = unit8_at<ROWS>(lens, a.batch, a.Hkv, a.G, next);
+        u = unit8_at(lens, a.batch, next);
         if (u.first < next) next = u.first + u.stages;
     }
     bool found = false;
@@ -577,7 +541,7 @@ merge8_kernel(const Attn8Args a, const __grid_constant__ BatchLens lens, const _
     while (found) {
         const int b0 = ra / KG, joints = (on ? rb - 1 : rb) / KG - b0 + 1, parts = joints + (on ? 1 : 0);
         auto row_of = [&](int p, int r) -> long { return (p < joints ? 2L * max(ra, (b0 + p) * KG) + 1 : 2L * rb) * ROWS + r; };
-        for (int r = blockIdx.y; r < min(ROWS, u.n * a.G - u.tile * ROWS); r += gridDim.y) {
+        for (int r = blockIdx.y; r < u.n * a.G; r += gridDim.y) {
             float top = -INFINITY, sum = 0.f;
             for (int p = lane; p < parts; p += 32) top = fmaxf(top, a.lse_part[row_of(p, r)]);
 #pragma unroll
@@ -601,7 +565,7 @@ merge8_kernel(const Attn8Args a, const __grid_constant__ BatchLens lens, const _
                     sum += s_sum[w];
                 }
                 const float by = 1.f / sum;
-                const long at = out_row8(a, lens, u, u.tile * ROWS + r);
+                const long at = out_row8(a, lens, u, r);
                 reinterpret_cast<uint2*>(a.out + at * 128)[lane] = make_uint2(ptx::pack_bf16x2(x.x * by, x.y * by), ptx::pack_bf16x2(x.z * by, x.w * by));
                 if (a.lse_out && lane == 0) a.lse_out[at] = (top + log2f(sum)) * kLn2;
             }

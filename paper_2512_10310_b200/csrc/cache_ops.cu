@@ -26,8 +26,8 @@ cudaError_t prepare_cache_kernels()
 {
     const std::pair<const void*, int> kernels[] = {{(const void*)attn8_kernel<1, 1>, Attn8Plan<1, 1>::kBytes},
                                                    {(const void*)attn8_kernel<2, 1>, Attn8Plan<2, 1>::kBytes},
-                                                   {(const void*)attn8_kernel<4, 1>, Attn8Plan<4, 1>::kBytes},
-                                                   {(const void*)attn8_kernel<4, 2>, Attn8Plan<4, 2>::kBytes},
+                                                   {(const void*)attn8_kernel<2, 2>, Attn8Plan<2, 2>::kBytes},
+                                                   {(const void*)attn8_kernel<2, 4>, Attn8Plan<2, 4>::kBytes},
                                                    {(const void*)key_weights_kernel<64>, KeyWeightPlan<64>::kBytes},
                                                    {(const void*)key_weights_kernel<128>, KeyWeightPlan<128>::kBytes},
                                                    {(const void*)select_keys_kernel, kSelectCache * 4}};
@@ -127,12 +127,14 @@ void batch_lens(BatchLens* bl, const evlnPagedParams* p, const int* lens, const 
 
 // ---- attention over the cache in 8 bits ----------------------------------------------------------
 
-// Most query rows of an episode (per kv head) that the kernel on the codes serves; more go through a bf16 copy.
-constexpr int kA8MostRows = 256;
+// Most query rows of an episode (per kv head) that the kernel on the codes serves: a tile's.  More go through a bf16 copy, which takes the same time for
+// 65 rows as for 250, less than the codes twice.  (us, 64, 128 and 256 rows on the codes, then through the copy: one episode of 4096 keys 17.1, 16.9 and
+// 21.7, 15.6 to 17.3; of 20656 28.2, 36.8, 59.2, 31.2 to 34.7; 16 of 8000 95.8, 175, 327, 139 to 140.)
+constexpr int kA8MostRows = 64;
 
 struct Plan8 {
     bool expand;
-    int most, rows;          // query rows of the longest episode (per kv head), of a tile: 8, 16, 32 or 64
+    int most, rows;          // query rows of the longest episode (per kv head), of a block: 8, 16, 32 or 64
     int run, total, runs, blocks;        // stages of a run, of the batch; runs, blocks
     int pages;               // expand: pages of the copy
     size_t copy_bytes;       // expand: table and pools
@@ -156,7 +158,7 @@ evlnStatus_t plan8(evlnHandle_t h, const evlnPagedParams* p, const int* lens, co
     for_episodes(p, lens, offs, [&](int, int L, int n) {
         if (n == 0) return;
         pages += ((long)L + n + kPage8 - 1) / kPage8;
-        total += ((long)n * G + pl->rows - 1) / pl->rows * p->num_kv_heads * (((long)L + n + kA8Keys - 1) / kA8Keys);
+        total += (long)p->num_kv_heads * (((long)L + n + kA8Keys - 1) / kA8Keys);
     });
     if (total > 0x3fffffffL || pages > 0x3fffffffL) return EVLN_NOT_SUPPORTED;
     if (pl->expand) {
@@ -166,7 +168,7 @@ evlnStatus_t plan8(evlnHandle_t h, const evlnPagedParams* p, const int* lens, co
     }
     // the SMs' key groups each a run of the same length
     const int groups = pl->rows == 8 ? Attn8Plan<1, 1>::kKeyGroups : pl->rows == 16 ? Attn8Plan<2, 1>::kKeyGroups
-                     : pl->rows == 32 ? Attn8Plan<4, 1>::kKeyGroups : Attn8Plan<4, 2>::kKeyGroups;
+                     : pl->rows == 32 ? Attn8Plan<2, 2>::kKeyGroups : Attn8Plan<2, 4>::kKeyGroups;
     pl->total = (int)total;
     pl->run = ceil_div(pl->total, h->num_sms * groups);
     if (pl->run < 1) pl->run = 1;
@@ -186,7 +188,7 @@ evlnPagedParams copy_params(const evlnPagedParams* p, const Plan8& pl)
 }
 
 template <int NQ, int RG>
-cudaError_t launch_attn8(const Plan8& pl, int most_rows, cudaStream_t st, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Attn8Args& a, const BatchLens& bl)
+cudaError_t launch_attn8(const Plan8& pl, cudaStream_t st, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Attn8Args& a, const BatchLens& bl)
 {
     using Plan = Attn8Plan<NQ, RG>;
     cudaError_t e = launch_pdl(attn8_kernel<NQ, RG>, dim3(pl.blocks), dim3(Plan::kThreads), Plan::kBytes, st, tm_k, tm_v, a, bl);
@@ -201,8 +203,7 @@ cudaError_t launch_attn8(const Plan8& pl, int most_rows, cudaStream_t st, const 
         }
         const bool few = list.count <= kMergeUnits;
         if (!few) list.count = 0;
-        const int rows = most_rows < Plan::kRows ? most_rows : Plan::kRows;
-        e = launch_pdl(merge8_kernel<Plan::kRows, Plan::kKeyGroups>, dim3(few ? list.count : pl.blocks, few || rows < 16 ? rows : 16), dim3(128), 0, st, a, bl, list);
+        e = launch_pdl(merge8_kernel<Plan::kRows, Plan::kKeyGroups>, dim3(few ? list.count : pl.blocks, few || pl.most < 16 ? pl.most : 16), dim3(128), 0, st, a, bl, list);
     }
     return e;
 }
@@ -361,8 +362,7 @@ evlnStatus_t evlnPaged8StepAttention(evlnHandle_t h, const evlnPagedParams* p, c
         void* inner = (char*)workspace + pl.copy_bytes;
         s = launched(h, launch_pdl(expand8_kernel, dim3((unsigned)pl.pages, (unsigned)hkv, 2), dim3(256), 0, st, a, bl));
         if (s == EVLN_OK)
-            s = evlnPagedStepAttention(h, &c, q_rot, a.k_out, a.v_out, h_cache_lens, h_new_offsets, a.out_table, inner, workspace_bytes - pl.copy_bytes, stream);
-        if (s == EVLN_OK) s = evlnPagedStepCombine(h, &c, inner, h_cache_lens, h_new_offsets, out, lse_out, stream);
+            s = paged_attention_to(h, &c, q_rot, a.k_out, a.v_out, h_cache_lens, h_new_offsets, a.out_table, inner, workspace_bytes - pl.copy_bytes, out, lse_out, stream);
         return s;
     }
 
@@ -371,7 +371,7 @@ evlnStatus_t evlnPaged8StepAttention(evlnHandle_t h, const evlnPagedParams* p, c
         bl.item_off[b] = at;
         if (b >= p->batch) continue;
         const int L = h_cache_lens[b], n = h_new_offsets[b + 1] - h_new_offsets[b];
-        if (n > 0) at += ceil_div(n * G, pl.rows) * hkv * ceil_div(L + n, kA8Keys);
+        if (n > 0) at += hkv * ceil_div(L + n, kA8Keys);
     }
     CUtensorMap tm_k, tm_v;
     const cuuint64_t dims[2] = {128, (cuuint64_t)p->num_pages * hkv * kPage8}, strides[1] = {128};
@@ -391,10 +391,10 @@ evlnStatus_t evlnPaged8StepAttention(evlnHandle_t h, const evlnPagedParams* p, c
     a.run = pl.run; a.total = pl.total;
     a.scale_log2 = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf(128.f)) * 1.4426950408889634f;
     a.div_g = make_fast_div((uint32_t)G);
-    return launched(h, pl.rows == 8    ? launch_attn8<1, 1>(pl, pl.most, st, tm_k, tm_v, a, bl)
-                       : pl.rows == 16 ? launch_attn8<2, 1>(pl, pl.most, st, tm_k, tm_v, a, bl)
-                       : pl.rows == 32 ? launch_attn8<4, 1>(pl, pl.most, st, tm_k, tm_v, a, bl)
-                                       : launch_attn8<4, 2>(pl, pl.most, st, tm_k, tm_v, a, bl));
+    return launched(h, pl.rows == 8    ? launch_attn8<1, 1>(pl, st, tm_k, tm_v, a, bl)
+                       : pl.rows == 16 ? launch_attn8<2, 1>(pl, st, tm_k, tm_v, a, bl)
+                       : pl.rows == 32 ? launch_attn8<2, 2>(pl, st, tm_k, tm_v, a, bl)
+                                       : launch_attn8<2, 4>(pl, st, tm_k, tm_v, a, bl));
 }
 
 // ---- eviction --------------------------------------------------------------------------------

@@ -146,6 +146,10 @@ inline bool encode_map(evlnHandle_t h, CUtensorMap* map, const void* base, int r
     return r == CUDA_SUCCESS;
 }
 
+// evlnPagedStepAttention + evlnPagedStepCombine in one (evln_api.cu).
+evlnStatus_t paged_attention_to(evlnHandle_t h, const evlnPagedParams* p, const void* q_rot, const void* k_pool, const void* v_pool, const int* h_cache_lens,
+                                const int* h_new_offsets, const int* d_page_table, void* workspace, size_t workspace_bytes, void* out, float* lse_out, void* stream);
+
 // Shared-memory limits of the kernels in cache_ops.cu, on the current device.
 cudaError_t prepare_cache_kernels();
 

@@ -1491,10 +1491,10 @@ evlnStatus_t evlnPagedRopeAppend(evlnHandle_t h, const evlnPagedParams* p, const
     return e == cudaSuccess ? EVLN_OK : cuda_fail(h, e);
 }
 
-evlnStatus_t evlnPagedStepAttention(evlnHandle_t h, const evlnPagedParams* p, const void* q_rot,
-                                    const void* k_pool, const void* v_pool, const int* h_cache_lens,
-                                    const int* h_new_offsets, const int* d_page_table, void* workspace,
-                                    size_t workspace_bytes, void* stream)
+// out: where rows that no split cuts go as they come from the tensor cores (bf16, with lse_out), null: to the workspace, for the combine call.
+static evlnStatus_t paged_attention(evlnHandle_t h, const evlnPagedParams* p, const void* q_rot, const void* k_pool, const void* v_pool,
+                                    const int* h_cache_lens, const int* h_new_offsets, const int* d_page_table, void* workspace,
+                                    size_t workspace_bytes, void* out, float* lse_out, void* stream)
 {
     evlnStatus_t s = check_paged_params(h, p, h_cache_lens, h_new_offsets);
     if (s != EVLN_OK) return s;
@@ -1583,8 +1583,8 @@ evlnStatus_t evlnPagedStepAttention(evlnHandle_t h, const evlnPagedParams* p, co
     }
     TcOutArgs d = {};
     if (smax == 1) {
-        d.out = (__nv_bfloat16*)workspace;
-        d.lse_out = a.lse_part;
+        d.out = (__nv_bfloat16*)(out ? out : workspace);
+        d.lse_out = out ? lse_out : a.lse_part;
     }
     if (items <= persistent_pairs(h, items)) {
         const cudaError_t e = launch_pair_pdl(attn_paged_pair_kernel, dim3(2 * (unsigned)items), kTcSmemBytes, (cudaStream_t)stream, tm_q, tm_k, tm_v, a, bl, d);
@@ -1611,6 +1611,14 @@ evlnStatus_t evlnPagedStepAttention(evlnHandle_t h, const evlnPagedParams* p, co
     return launch_persistent(h, items, d, table, [&](dim3 grid) {
         return launch_pair_pdl(attn_persistent_kernel<true, PagedLens>, grid, kPersistSmemBytes, (cudaStream_t)stream, tm_q, tm_k, tm_v, a, bl, d, table);
     });
+}
+
+evlnStatus_t evlnPagedStepAttention(evlnHandle_t h, const evlnPagedParams* p, const void* q_rot,
+                                    const void* k_pool, const void* v_pool, const int* h_cache_lens,
+                                    const int* h_new_offsets, const int* d_page_table, void* workspace,
+                                    size_t workspace_bytes, void* stream)
+{
+    return paged_attention(h, p, q_rot, k_pool, v_pool, h_cache_lens, h_new_offsets, d_page_table, workspace, workspace_bytes, nullptr, nullptr, stream);
 }
 
 evlnStatus_t evlnPagedStepCombine(evlnHandle_t h, const evlnPagedParams* p, const void* workspace,
@@ -1668,6 +1676,18 @@ evlnStatus_t evlnPagedCheckTable(const evlnPagedParams* p, const int* h_cache_le
 }
 
 }  // extern "C"
+
+// Attention and combine in one call (the 8-bit cache's bf16 copy): unsplit rows go straight to the caller's output.
+evlnStatus_t evln::paged_attention_to(evlnHandle_t h, const evlnPagedParams* p, const void* q_rot, const void* k_pool, const void* v_pool,
+                                      const int* h_cache_lens, const int* h_new_offsets, const int* d_page_table, void* workspace, size_t workspace_bytes,
+                                      void* out, float* lse_out, void* stream)
+{
+    const evlnStatus_t s = paged_attention(h, p, q_rot, k_pool, v_pool, h_cache_lens, h_new_offsets, d_page_table, workspace, workspace_bytes, out, lse_out, stream);
+    if (s != EVLN_OK) return s;
+    const PagedPlan plan = paged_schedule(h, p, h_cache_lens, h_new_offsets);
+    if (plan.splits == 1 && !plan.few) return EVLN_OK;
+    return evlnPagedStepCombine(h, p, workspace, h_cache_lens, h_new_offsets, out, lse_out, stream);
+}
 
 // ---- packed sequence under the action-isolating mask (Sec. 3.3) -----------------------------
 

@@ -9,8 +9,9 @@ from tests.helpers import f64
 
 pytestmark = pytest.mark.gpu
 DEV, P, D, THETA, EPS = "cuda:0", 64, 128, 1.0e6, 1e-6
-# Attention, relative to sum p |v| (p the exact probabilities): on the codes p is rounded to halves (2^-11), through the bf16 copy to
-# bf16 (2^-8) with an exponential good to 2^-13; fp32 scores of a few dozen are off by under 2^-15 of p.  Then the output's rounding, 2^-8.
+# Attention, relative to sum p |v| (p the exact probabilities): on the codes (up to 64 rows per kv head in every episode) p is rounded to halves (2^-11),
+# through the bf16 copy to bf16 (2^-8) with an exponential good to 2^-13; fp32 scores of a few dozen are off by under 2^-15 of p.  Then the output's
+# rounding, 2^-8.
 P_ERROR = {"codes": 2.0 ** -11 + 2.0 ** -14, "copy": 2.0 ** -8 + 2.0 ** -12}
 LSE_ERROR = {"codes": 2.0 ** -14, "copy": 1e-3}
 
@@ -86,7 +87,12 @@ class Batch:
         assert B.evlnGetDeviceStatus(self.h) == 0
         return out, lse
 
-    def check(self, q_rot, out, lse, kind):
+    @property
+    def kind(self):
+        return "codes" if max(self.news) * self.G <= 64 else "copy"
+
+    def check(self, q_rot, out, lse):
+        kind = self.kind
         q = f64(q_rot).reshape(self.hkv, -1, self.G, D).transpose(1, 0, 2, 3).reshape(-1, self.hq, D)
         for b, L in enumerate(self.lens):
             rows = slice(self.offs[b], self.offs[b + 1])
@@ -193,7 +199,7 @@ def test_a_page_filled_token_by_token(handle):
 
 
 ATTENDS = [
-    # rows per kv head: 1 .. 16, .. 32, .. 64 and several tiles of 64; lengths of one token, ends of pages and stages
+    # rows per kv head: up to 8, 16, 32, 64 and more; lengths of one token, ends of pages and stages
     ([0], [1], 2, 1), ([31], [1], 2, 1), ([32], [1], 28, 4), ([63, 64, 65, 0], [1, 1, 1, 1], 28, 4),
     ([1000, 1, 4095, 130], [1, 2, 1, 0], 28, 4), ([777, 64], [4, 3], 28, 4), ([500], [9], 28, 4), ([95, 2000, 7], [8, 20, 30], 28, 4),
     ([8191], [1], 64, 8), ([0, 100], [33, 17], 8, 8), ([1500], [256], 3, 3), ([300], [1], 40, 1), ([5, 6], [11, 1], 12, 1),
@@ -206,9 +212,10 @@ def test_attention_on_the_codes(handle, lens, news, hq, hkv):
     x.fill_new()
     q_rot = x.q_rot()
     out, lse = x.attend(q_rot)
-    x.check(q_rot, out, lse, "codes")
-    again = x.attend(q_rot)
-    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    x.check(q_rot, out, lse)
+    if x.kind == "codes":      # (on CTA pairs a row's softmax reference may move, and where to depends on who noticed first)
+        again = x.attend(q_rot)
+        assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
 
 
 @pytest.mark.parametrize("lens,news,hq,hkv", [([0, 63, 64, 333, 1000], [70, 1, 129, 0, 196], 28, 4), ([50], [300], 1, 1), ([4096], [196], 28, 4)])
@@ -217,7 +224,7 @@ def test_attention_through_the_copy(handle, lens, news, hq, hkv):
     x.fill_new()
     q_rot = x.q_rot()
     out, lse = x.attend(q_rot)
-    x.check(q_rot, out, lse, "copy")
+    x.check(q_rot, out, lse)
 
 
 def test_attention_many_short_episodes_and_more_units_than_blocks(handle):
@@ -226,7 +233,7 @@ def test_attention_many_short_episodes_and_more_units_than_blocks(handle):
     x.fill_new()
     q_rot = x.q_rot()
     out, lse = x.attend(q_rot)
-    x.check(q_rot, out, lse, "codes")
+    x.check(q_rot, out, lse)
 
 
 @pytest.mark.parametrize("q_size,scale", [(40.0, 0.0), (1e-3, 0.0), (1.5, 2.0), (3.0e30, 1e-30)])
@@ -256,7 +263,7 @@ def test_value_scales_far_apart(handle):
             x.scales[1][x.rows[0][i]] = 2.0 ** e
         q_rot = x.q_rot()
         out, lse = x.attend(q_rot)
-        x.check(q_rot, out, lse, "codes")
+        x.check(q_rot, out, lse)
 
 
 def test_what_is_not_finite_stays_with_its_rows(handle):
