@@ -6,10 +6,12 @@
 // follows exact: code * scale is a bf16 number, and a page that fills up token by token can be rounded anew when a larger
 // token arrives: codes that stay normal numbers only change their exponents, so no error piles up.
 //
-// append8_kernel: a block for every (touched page, kv head, keys or values), and blocks for the tokens' queries.  A page
-// block holds its tokens (8 lanes a token, 16 channels a lane) in registers from the load over norm, rotation and the block's
-// maximum to the codes: one pass.  Codes of earlier tokens are loaded instead of new ones and stored again only if the scale grew.
-// Bound: latency for a token an episode (a chain of loads, the block's maximum, stores), else the queries' traffic.
+// append8_kernel: a block for every (touched page, kv head, keys or values), and blocks for the tokens' queries (warps as in
+// head_norm.cuh).  A page block holds its tokens (8 lanes and 16 channels a lane for each, two tokens a lane) in registers from the load over
+// norm, rotation and the block's maximum to the codes: one pass.  Codes of earlier tokens are loaded instead of new ones and stored again only
+// if the scale grew.
+// Bound: latency for a token an episode (a chain of loads, the block's maximum, stores: 16 episodes 2.4 us), else the queries' traffic (16 frames of
+// 196 tokens with norms, 56 MB, 18.1 us).  (One token a lane, blocks of 512 threads: 2.7 and 21.4 us.)
 #pragma once
 
 #include <cuda_fp16.h>
@@ -21,8 +23,7 @@
 
 namespace evln {
 
-constexpr int kPage8 = 64, kAppend8Threads = 8 * kPage8;
-constexpr int kAppend8Tokens = 16;                     // most tokens of a query block
+constexpr int kPage8 = 64, kAppend8Threads = 4 * kPage8, kAppend8Blocks = 3;
 constexpr int kScaleMin8 = -120, kScaleMax8 = 120;     // exponents; a page of zeros has the least scale
 
 struct Append8Args {
@@ -31,9 +32,8 @@ struct Append8Args {
     float* k_scale;          // [pages, Hkv]
     float* v_scale;
     int page_blocks;         // touched pages * Hkv
-    int q_threads;           // threads per token for its queries (whole warps); a block takes kAppend8Threads / q_threads tokens
-    int q_tokens;            // ... of them
-    FastDiv div_hkv;
+    int q_warps;             // warps per token for its queries
+    FastDiv div_hkv, div_warps;
 };
 
 __device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
@@ -46,13 +46,6 @@ __device__ __forceinline__ int scale_exponent8(float most)
     return e < kScaleMin8 ? kScaleMin8 : e > kScaleMax8 ? kScaleMax8 : e;
 }
 
-// |x| for the page's maximum: infinities and NaN do not count (an infinity becomes the largest code, NaN a NaN code)
-__device__ __forceinline__ float finite_abs(float x)
-{
-    const float m = fabsf(x);
-    return m < INFINITY ? m : 0.f;
-}
-
 // floats to codes (nearest, ties to even; beyond 448 the largest code)
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d)
 {
@@ -61,9 +54,14 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d)
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
     return (uint32_t)lo | ((uint32_t)hi << 16);
 }
-__device__ __forceinline__ uint2 codes8(const float (&x)[8], float inv)
+// eight floats (four pairs) times down to codes
+__device__ __forceinline__ uint2 codes8(const uint64_t (&x)[4], float down)
 {
-    return make_uint2(codes4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv), codes4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv));
+    const uint64_t d = ptx::pack2(down, down);
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ptx::unpack2(ptx::mul2(x[i], d), f[2 * i], f[2 * i + 1]);
+    return make_uint2(codes4(f[0], f[1], f[2], f[3]), codes4(f[4], f[5], f[6], f[7]));
 }
 // four codes to four halves, exactly (NaN stays NaN)
 __device__ __forceinline__ void halves4(uint32_t codes, uint32_t& lo, uint32_t& hi)
@@ -79,58 +77,38 @@ __device__ __forceinline__ void floats4(uint32_t codes, float* x)
     x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
 }
 
-template <bool NORM>
-__global__ void __launch_bounds__(kAppend8Threads, 2)
+template <bool NORM, bool TABLE>
+__global__ void __launch_bounds__(kAppend8Threads, kAppend8Blocks)
 append8_kernel(const Append8Args p, const __grid_constant__ BatchLens lens)
 {
     typedef __nv_bfloat16 T;
     constexpr int D = 128, half = 64, kVectors = 8;        // vector pairs of a head
-    __shared__ __align__(16) TokenAngles<T, NORM> s_angles[kAppend8Tokens];
-    __shared__ float s_most[kAppend8Threads / 32];
+    constexpr int kWarps = kAppend8Threads / 32;
+    __shared__ union {
+        TokenAngles<T, NORM> of_token[kWarps];             // queries: a warp's token
+        TokenAngles<T, true> of_slots[kWarps][4];          // keys: a warp's four tokens
+    } s_angles;
+    __shared__ float s_most[kWarps];
     const RopeArgs& a = p.r;
     const int blk = blockIdx.x, k = threadIdx.x & (kVectors - 1), c0 = k * 8;      // a lane's channels: c0 .. and c0 + 64 ..
     if (blk >= 2 * p.page_blocks) {
-        // ---- queries of a few tokens ----
-        const int tok0 = (blk - 2 * p.page_blocks) * p.q_tokens, tokens = min(p.q_tokens, a.num_new - tok0);
-        auto position = [&](int tok) -> int {
+        // ---- queries: q_warps warps per token ----
+        const int wid = threadIdx.x >> 5, w = (blk - 2 * p.page_blocks) * kWarps + wid, tok = (int)fast_div((uint32_t)w, p.div_warps);
+        double omega[2];
+        own_omegas<TABLE>(a, omega);
+        ptx::grid_dependency_wait();
+        ptx::grid_launch_dependents();
+        if (tok >= a.num_new) return;
+        const int items = a.Hq * kVectors;
+        token_heads<T, NORM>(a, p.norm, s_angles.of_token[wid], tok, 32 * (w - tok * p.q_warps) + (threadIdx.x & 31), 32 * p.q_warps, items, items, items, 0, [&]() -> long {
             int b = 0, hi = a.batch;                          // largest b with new_off[b] <= tok
             while (hi - b > 1) {
                 const int mid = (b + hi) >> 1;
                 if (lens.new_off[mid] <= tok) b = mid; else hi = mid;
             }
-            return lens.cache_len[b] + tok - lens.new_off[b];
-        };
-        const double omega = a.table ? 0.0 : rope_omega(threadIdx.x & (half - 1), D, a.log2_theta);
-        const int group = threadIdx.x / p.q_threads, tok = tok0 + group, items = a.Hq * kVectors;
-        ptx::grid_dependency_wait();
-        ptx::grid_launch_dependents();
-        int it = threadIdx.x - group * p.q_threads;
-        const bool there = group < tokens;
-        const T* src = (const T*)a.q_new + tok * a.q_stride + c0;
-        uint4 r0 = make_uint4(0u, 0u, 0u, 0u), r1 = r0;
-        auto load = [&]() {
-            if (there && it < items) {
-                r0 = *reinterpret_cast<const uint4*>(src + (it / kVectors) * D);
-                r1 = *reinterpret_cast<const uint4*>(src + (it / kVectors) * D + half);
-            }
-        };
-        load();                                               // in flight while the angles arrive
-        for (int e = threadIdx.x; e < tokens * half; e += kAppend8Threads) {
-            const int j = e & (half - 1), pos = position(tok0 + e / half);
-            s_angles[e / half].put(j, a.table ? a.table[(long)(pos - a.table_first) * half + j] : rope_cos_sin_at(pos, omega));
-        }
-        __syncthreads();
-        if (!there) return;                                   // (whole warps)
-        for (; it - (int)(threadIdx.x & 31) < items; it += p.q_threads, load()) {
-            uint4 y0, y1;
-            if constexpr (NORM) norm_turn<T>(s_angles[group], k, 3, D, p.norm.eps, (const T*)p.norm.q_weight, r0, r1, y0, y1);
-            else Rotation<T>::turn(s_angles[group].at, k, r0, r1, y0, y1);
-            if (it >= items) continue;
-            const int h = it / kVectors, g = (int)fast_div((uint32_t)h, a.div_g);
-            T* dst = (T*)a.q_rot + ((long)g * a.num_new * a.G + (long)tok * a.G + (h - g * a.G)) * D + c0;
-            *reinterpret_cast<uint4*>(dst) = y0;
-            *reinterpret_cast<uint4*>(dst + half) = y1;
-        }
+            fill_angles<TABLE>(s_angles.of_token[wid], a, lens.cache_len[b] + tok - lens.new_off[b], omega);
+            return 0;
+        });
         return;
     }
     // ---- a page of one kv head: keys (first, they have the longer chain) or values ----
@@ -144,73 +122,105 @@ append8_kernel(const Append8Args p, const __grid_constant__ BatchLens lens)
     }
     const int L = lens.cache_len[b], off = lens.new_off[b], n = lens.new_off[b + 1] - off;
     const int p0 = (L / kPage8 + pg - lens.item_off[b]) * kPage8;          // position of the page's first slot
-    const int slot = threadIdx.x / kVectors, pos = p0 + slot;
-    const bool is_old = pos < L, is_new = pos >= L && pos < L + n, held = p0 < L;
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, slot0 = threadIdx.x / kVectors;      // a lane's slots: slot0 and slot0 + 32
+    const bool held = p0 < L;
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     const int page = a.page_table[(long)b * a.max_pages + p0 / kPage8];
-    uint8_t* at = (uint8_t*)(is_v ? a.v_cache : a.k_cache) + (((long)page * a.Hkv + g) * kPage8 + slot) * D + c0;
+    uint8_t* const at = (uint8_t*)(is_v ? a.v_cache : a.k_cache) + (((long)page * a.Hkv + g) * kPage8 + slot0) * D + c0;
     float* scale_at = (is_v ? p.v_scale : p.k_scale) + (long)page * a.Hkv + g;
+    auto is_old = [&](int u) { return p0 + slot0 + 32 * u < L; };
+    auto is_new = [&](int u) { const int pos = p0 + slot0 + 32 * u; return pos >= L && pos < L + n; };
 
-    uint4 r0 = make_uint4(0u, 0u, 0u, 0u), r1 = r0;       // a new token's 16 numbers, or an earlier one's 16 codes
-    if (is_new) {
-        const long tok = off + pos - L;
-        const T* src = (is_v ? (const T*)a.v_new + tok * a.v_stride : (const T*)a.k_new + tok * a.k_stride) + (long)g * D + c0;
-        r0 = *reinterpret_cast<const uint4*>(src);
-        r1 = *reinterpret_cast<const uint4*>(src + half);
-    } else if (is_old) {
-        const uint2 lo = *reinterpret_cast<const uint2*>(at), hi8 = *reinterpret_cast<const uint2*>(at + half);
-        r0 = make_uint4(lo.x, lo.y, hi8.x, hi8.y);
+    uint4 r0[2], r1[2];                                   // a new token's 16 numbers, or an earlier one's 16 codes
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        r0[u] = r1[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (is_new(u)) {
+            const long tok = off + p0 + slot0 + 32 * u - L;
+            const T* src = (is_v ? (const T*)a.v_new + tok * a.v_stride : (const T*)a.k_new + tok * a.k_stride) + (long)g * D + c0;
+            r0[u] = *reinterpret_cast<const uint4*>(src);
+            r1[u] = *reinterpret_cast<const uint4*>(src + half);
+        } else if (is_old(u)) {
+            const uint2 lo = *reinterpret_cast<const uint2*>(at + 32 * u * D), hi8 = *reinterpret_cast<const uint2*>(at + 32 * u * D + half);
+            r0[u] = make_uint4(lo.x, lo.y, hi8.x, hi8.y);
+        }
     }
     const float old_scale = held ? *scale_at : 0.f;
-    float x[2][8], most = 0.f;
-    float inv = 1.f;
-    if (NORM && !is_v) inv = norm_factor<T>(r0, r1, 3, D, p.norm.eps);
-    if (is_new) {
-        to_floats<T, 8>(r0, x[0]);
-        to_floats<T, 8>(r1, x[1]);
-        if (!is_v) {
-            if (NORM) {
-                const T* w = (const T*)p.norm.k_weight;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x[0][i] *= inv * (w ? to_float(w[c0 + i]) : 1.f);
-                    x[1][i] *= inv * (w ? to_float(w[c0 + half + i]) : 1.f);
-                }
-            }
-            // every angle of a token serves one pair of this head, so the lanes take them straight from the table
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const double2 cs = a.table ? a.table[(long)(pos - a.table_first) * half + c0 + i] : rope_cos_sin(pos, c0 + i, D, a.log2_theta);
-                const float c = (float)cs.x, s = (float)cs.y, u = x[0][i], v = x[1][i];
-                x[0][i] = fmaf(u, c, -(v * s));
-                x[1][i] = fmaf(v, c, u * s);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) most = fmaxf(most, fmaxf(finite_abs(x[0][i]), finite_abs(x[1][i])));
+    uint64_t x[2][2][4];                                  // the numbers to store, in pairs
+    uint4 w0 = make_uint4(0u, 0u, 0u, 0u), w1 = w0;
+    const bool weighted = NORM && !is_v && p.norm.k_weight;
+    if (weighted) {
+        w0 = *reinterpret_cast<const uint4*>((const T*)p.norm.k_weight + c0);
+        w1 = *reinterpret_cast<const uint4*>((const T*)p.norm.k_weight + c0 + half);
     }
 #pragma unroll
-    for (int s = 16; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
-    if ((threadIdx.x & 31) == 0) s_most[threadIdx.x >> 5] = most;
-    __syncthreads();
-    most = s_most[threadIdx.x & (kAppend8Threads / 32 - 1)];
+    for (int u = 0; u < 2; ++u) {
+        if (is_v) {
 #pragma unroll
-    for (int s = kAppend8Threads / 64; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
+            for (int i = 0; i < 4; ++i) {
+                x[u][0][i] = pair_of<T>(r0[u], i);
+                x[u][1][i] = pair_of<T>(r1[u], i);
+            }
+            continue;
+        }
+        // the angles of the warp's four tokens (an angle serves one pair of this head)
+        const int first = p0 + 32 * u + 4 * wid;          // position of the first
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int j = (lane + 32 * i) & (half - 1), pos = first + i / 2;
+            if (pos >= L && pos < L + n) s_angles.of_slots[wid][i / 2].put(j, TABLE ? a.table[(long)(pos - a.table_first) * half + j] : rope_cos_sin(pos, j, D, a.log2_theta));
+        }
+        __syncwarp();
+        const float inv = NORM ? norm_factor<T>(r0[u], r1[u], 3, D, p.norm.eps) : 1.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) norm_turn_pair<T>(s_angles.of_slots[wid][slot0 & 3], k, i, inv, weighted, w0, w1, r0[u], r1[u], x[u][0][i], x[u][1][i]);
+    }
+    // the page's maximum; infinities and NaN do not count (an infinity becomes the largest code, NaN a NaN code)
+    float most = 0.f;
+    auto meet = [&](auto size) {
+        most = 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            if (is_new(u)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float lo, hi;
+                    ptx::unpack2(x[u][i >> 2][i & 3], lo, hi);
+                    most = ptx::max3(most, size(lo), size(hi));
+                }
+            }
+    };
+    meet([](float v) { return fabsf(v); });               // (the maximum of a number and NaN is the number)
+    if (most == INFINITY) meet([](float v) { return fabsf(v) < INFINITY ? fabsf(v) : 0.f; });
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
+    if (lane == 0) s_most[wid] = most;
+    __syncthreads();
+    most = s_most[lane & (kWarps - 1)];
+#pragma unroll
+    for (int s = kWarps / 2; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
     const float need = exp2_int(scale_exponent8(most)), scale = held && old_scale > need ? old_scale : need;
     const bool grew = held && scale > old_scale;
-    const float down = 1.f / scale;                        // powers of two: exact
-    if (is_old && grew) {
-        const float again = old_scale * down;
-        floats4(r0.x, x[0]); floats4(r0.y, x[0] + 4);
-        floats4(r0.z, x[1]); floats4(r0.w, x[1] + 4);
-        *reinterpret_cast<uint2*>(at) = codes8(x[0], again);
-        *reinterpret_cast<uint2*>(at + half) = codes8(x[1], again);
-    } else if (is_new) {
-        *reinterpret_cast<uint2*>(at) = codes8(x[0], down);
-        *reinterpret_cast<uint2*>(at + half) = codes8(x[1], down);
-    } else if (is_v && !is_old) {
-        *reinterpret_cast<uint2*>(at) = *reinterpret_cast<uint2*>(at + half) = make_uint2(0u, 0u);      // behind the last token: nothing that could be NaN
+    const float down = 1.f / scale;                       // powers of two: exact
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        uint2* const to = reinterpret_cast<uint2*>(at + 32 * u * D);
+        if (is_old(u)) {
+            if (!grew) continue;
+            float f[16];
+            floats4(r0[u].x, f); floats4(r0[u].y, f + 4); floats4(r0[u].z, f + 8); floats4(r0[u].w, f + 12);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[u][i >> 2][i & 3] = ptx::pack2(f[2 * i], f[2 * i + 1]);
+            to[0] = codes8(x[u][0], old_scale * down);
+            to[half / 8] = codes8(x[u][1], old_scale * down);
+        } else if (is_new(u)) {
+            to[0] = codes8(x[u][0], down);
+            to[half / 8] = codes8(x[u][1], down);
+        } else if (is_v) {
+            to[0] = to[half / 8] = make_uint2(0u, 0u);    // behind the last token: nothing that could be NaN
+        }
     }
     if (threadIdx.x == 0 && (!held || grew)) *scale_at = scale;
 }

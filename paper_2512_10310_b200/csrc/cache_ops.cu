@@ -110,12 +110,27 @@ NormArgs norm_args(const evlnHeadNorm* norm)
     return n;
 }
 
-// A block per token with a thread per work item, as for the append without norms; few tokens of many heads get several.
-dim3 token_grid(int tokens, int extra, int items, dim3* block)
+// Warps per token for its items: one for each 32 of them while all are resident at once (so many that the GPU has room for), else fewer.
+int token_warps(long tokens, int items, long room)
 {
-    const int parts = tokens <= kRopeFewTokens ? ceil_div(items, kRopeThreadsMax) : 1, t = (ceil_div(items, parts) + 31) / 32 * 32;
-    *block = dim3(t > kRopeThreadsMax ? kRopeThreadsMax : t < 64 ? 64 : t);
-    return dim3((unsigned)(tokens + extra), (unsigned)parts);
+    const int most = ceil_div(items, 32);
+    const long fill = room / tokens;
+    return fill >= most ? most : fill < 1 ? 1 : (int)fill;
+}
+
+// Launches the append with the norms; extra: warps behind the tokens'.
+template <typename T, bool PAGED, typename LensT>
+evlnStatus_t launch_norm_append(evlnHandle_t h, const RopeArgs& a, const evlnHeadNorm* norm, int extra, const LensT& lens, void* stream)
+{
+    const int items = ((a.Hq + a.Hkv) << a.vph_shift) + (a.Hkv << (a.vph_shift + 1));
+    const int warps = token_warps(a.num_new, items, (long)h->num_sms * kNormWarps * kNormBlocks - extra);
+    const long blocks = ((long)a.num_new * warps + extra + kNormWarps - 1) / kNormWarps;
+    if (blocks > 0x7fffffL) return EVLN_NOT_SUPPORTED;
+    auto launch = [&](auto kernel) {
+        return launched(h, launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * kNormWarps), 0, (cudaStream_t)stream, a, norm_args(norm), warps,
+                                      make_fast_div((uint32_t)warps), lens));
+    };
+    return a.table ? launch(norm_append_kernel<T, PAGED, true, LensT>) : launch(norm_append_kernel<T, PAGED, false, LensT>);
 }
 
 void batch_lens(BatchLens* bl, const evlnPagedParams* p, const int* lens, const int* offs)
@@ -229,12 +244,8 @@ evlnStatus_t evlnNormRopeAppend(evlnHandle_t h, const evlnStepParams* p, const e
                             p->rope_table, p->rope_table_first_pos);
     a.q_rot = q_rot; a.k_cache = k_cache; a.v_cache = v_cache;
     a.cache_len = p->cache_len; a.num_new = p->num_new; a.cache_cap = p->cache_capacity;
-    dim3 block;
-    const dim3 grid = token_grid(p->num_new, 0, ((a.Hq + a.Hkv) << a.vph_shift) + (a.Hkv << (a.vph_shift + 1)), &block);
-    const NoLens nl = {};
-    const NormArgs n = norm_args(norm);
-    return launched(h, p->dtype == EVLN_BF16 ? launch_pdl(norm_append_kernel<__nv_bfloat16, false, NoLens>, grid, block, 0, (cudaStream_t)stream, a, n, nl)
-                                             : launch_pdl(norm_append_kernel<float, false, NoLens>, grid, block, 0, (cudaStream_t)stream, a, n, nl));
+    return p->dtype == EVLN_BF16 ? launch_norm_append<__nv_bfloat16, false>(h, a, norm, 0, NoLens(), stream)
+                                 : launch_norm_append<float, false>(h, a, norm, 0, NoLens(), stream);
 }
 
 evlnStatus_t evlnPagedNormRopeAppend(evlnHandle_t h, const evlnPagedParams* p, const evlnHeadNorm* norm, const void* q_new, const void* k_new,
@@ -257,9 +268,7 @@ evlnStatus_t evlnPagedNormRopeAppend(evlnHandle_t h, const evlnPagedParams* p, c
     while ((1 << a.page_shift) < a.page_size) ++a.page_shift;
     BatchLens bl;
     batch_lens(&bl, p, h_cache_lens, h_new_offsets);
-    dim3 block;
-    const dim3 grid = token_grid(total, p->batch, ((a.Hq + a.Hkv) << a.vph_shift) + (a.Hkv << (a.vph_shift + 1)), &block);
-    return launched(h, launch_pdl(norm_append_kernel<__nv_bfloat16, true, BatchLens>, grid, block, 0, (cudaStream_t)stream, a, norm_args(norm), bl));
+    return launch_norm_append<__nv_bfloat16, true>(h, a, norm, p->batch * a.Hkv, bl, stream);
 }
 
 evlnStatus_t evlnPaged8RopeAppend(evlnHandle_t h, const evlnPagedParams* p, const evlnHeadNorm* norm, const void* q_new, const void* k_new,
@@ -292,15 +301,15 @@ evlnStatus_t evlnPaged8RopeAppend(evlnHandle_t h, const evlnPagedParams* p, cons
         const int L = h_cache_lens[b], n = h_new_offsets[b + 1] - h_new_offsets[b];
         if (n > 0) pages += ((long)L + n + kPage8 - 1) / kPage8 - L / kPage8;
     }
-    a.q_threads = (a.r.Hq * 8 + 31) / 32 * 32;
-    if (a.q_threads > kAppend8Threads) a.q_threads = kAppend8Threads;
-    a.q_tokens = kAppend8Threads / a.q_threads;
-    const long blocks = 2 * pages * p->num_kv_heads + ((long)total + a.q_tokens - 1) / a.q_tokens;
+    a.q_warps = token_warps(total, a.r.Hq * 8, (long)h->num_sms * (kAppend8Threads / 32) * kAppend8Blocks);
+    a.div_warps = make_fast_div((uint32_t)a.q_warps);
+    const long blocks = 2 * pages * p->num_kv_heads + ((long)total * a.q_warps * 32 + kAppend8Threads - 1) / kAppend8Threads;
     if (blocks > 0x3fffffffL) return EVLN_NOT_SUPPORTED;
     a.page_blocks = (int)(pages * p->num_kv_heads);
     a.div_hkv = make_fast_div((uint32_t)p->num_kv_heads);
-    return launched(h, norm ? launch_pdl(append8_kernel<true>, dim3((unsigned)blocks), dim3(kAppend8Threads), 0, (cudaStream_t)stream, a, bl)
-                            : launch_pdl(append8_kernel<false>, dim3((unsigned)blocks), dim3(kAppend8Threads), 0, (cudaStream_t)stream, a, bl));
+    auto launch = [&](auto kernel) { return launched(h, launch_pdl(kernel, dim3((unsigned)blocks), dim3(kAppend8Threads), 0, (cudaStream_t)stream, a, bl)); };
+    if (a.r.table) return norm ? launch(append8_kernel<true, true>) : launch(append8_kernel<false, true>);
+    return norm ? launch(append8_kernel<true, false>) : launch(append8_kernel<false, false>);
 }
 
 evlnStatus_t evlnPaged8WorkspaceSize(evlnHandle_t h, const evlnPagedParams* p, const int* h_cache_lens, const int* h_new_offsets, size_t* bytes)

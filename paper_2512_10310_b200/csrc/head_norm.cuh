@@ -3,11 +3,14 @@
 //     y = w * x / sqrt(mean(x^2) + eps)       over the D channels of a head, queries and keys
 //
 // then the rotation of Sec. 3.2 at the token's position and the stores of rope_append.cuh.  A head vector is 2^s lanes of
-// one warp, a pair of 16-byte vectors (channels j.. and j + D/2..) each: the sum of squares is V FMAs a half and s
-// shuffles, and the pair is what the rotation wants.  Everything after the load is in floats and rounded once, to the
-// storage type: there is no rounding between norm and rotation, as there is where they are two passes.
-// Bound: as rope_append.cuh (latency for few tokens, then instructions and HBM); a norm adds one dependent chain of
-// shuffles and a square root to a token.
+// one warp, a pair of 16-byte vectors (channels j.. and j + D/2..) each: the sum of squares is V packed FMAs and s
+// shuffles, and the pair is what the rotation wants.  Everything after the load is in floats (two channels an instruction) and rounded once,
+// to the storage type: there is no rounding between norm and rotation, as there is where they are two passes.
+// A warp serves one token: it fills the token's angles into its own corner of shared memory, then takes 32 work items after the other, so that no
+// warp waits for another one and the angles' cost is shared.  As many warps per token as are resident together: a second wave costs more than a
+// longer loop (392 tokens of 28 + 8 heads: 9 warps each 4.1 us, 10 warps and two waves 6.2).
+// Bound: for few tokens latency (1.5 us for one), for many HBM: 3136 tokens, 58 MB, 15.2 us = 3.8 TB/s, where the same bytes take 10.4 us in an
+// elementwise pass.  (A block per token with a thread per item issued 2.5 times the instructions and took 19.8 us, blocks of two tokens 17.5.)
 #pragma once
 
 #include "common.cuh"
@@ -16,180 +19,227 @@
 
 namespace evln {
 
+// A block: four warps (of eight, the first of few tokens started later: 1.9 us for a token, 1.5).  The loop keeps 80 registers; with fewer, and so more
+// warps resident, the compiler puts some of it aside (3136 tokens: 15.0 us with 24 warps an SM, 16.4 with 28, 19.0 with 32).
+constexpr int kNormWarps = 4, kNormBlocks = 6;
+
 struct NormArgs {
     const void* q_weight;    // [D] of the tokens' type, or null: ones
     const void* k_weight;
     float eps;
 };
 
-// 16 bytes of T as floats and back (one rounding)
-template <typename T, int V>
-__device__ __forceinline__ void to_floats(const uint4& raw, float (&x)[V])
+// elements 2 i, 2 i + 1 of 16 bytes of T, as a pair of floats for the packed instructions, and back
+template <typename T>
+__device__ __forceinline__ uint64_t pair_of(const uint4& raw, int i)
 {
     const T* e = reinterpret_cast<const T*>(&raw);
-#pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = to_float(e[i]);
-}
-template <typename T, int V>
-__device__ __forceinline__ uint4 from_floats(const float (&x)[V])
-{
-    uint4 raw;
-    T* e = reinterpret_cast<T*>(&raw);
-#pragma unroll
-    for (int i = 0; i < V; ++i) from_float(x[i], e[i]);
-    return raw;
-}
-// elements 2 i, 2 i + 1 of 16 bytes
-template <typename T>
-__device__ __forceinline__ float2 pair_of(const uint4& raw, int i)
-{
-    const T* e = reinterpret_cast<const T*>(&raw);
-    return make_float2(to_float(e[2 * i]), to_float(e[2 * i + 1]));
+    return ptx::pack2(to_float(e[2 * i]), to_float(e[2 * i + 1]));
 }
 template <typename T>
-__device__ __forceinline__ void set_pair(uint4& raw, int i, float x, float y)
+__device__ __forceinline__ void set_pair(uint4& raw, int i, uint64_t v)
 {
+    float x, y;
+    ptx::unpack2(v, x, y);
     T* e = reinterpret_cast<T*>(&raw);
     from_float(x, e[2 * i]);
     from_float(y, e[2 * i + 1]);
 }
+template <>
+__device__ __forceinline__ void set_pair<__nv_bfloat16>(uint4& raw, int i, uint64_t v)
+{
+    float x, y;
+    ptx::unpack2(v, x, y);
+    reinterpret_cast<uint32_t*>(&raw)[i] = ptx::pack_bf16x2(x, y);
+}
 
-// 1 / sqrt(mean square + eps) of a head vector that 2^shift neighbouring lanes hold, lo and hi each (all lanes of the warp call this)
+// 1 / sqrt(mean square + eps) of a head vector that 2^shift neighbouring lanes hold, lo and hi each (all lanes of the warp call this).  D: 2^n.
 template <typename T>
 __device__ __forceinline__ float norm_factor(const uint4& lo, const uint4& hi, int shift, int D, float eps)
 {
-    float ss = 0.f;
+    uint64_t ss2 = 0;
 #pragma unroll
     for (int i = 0; i < VecTraits<T>::kVec / 2; ++i) {
-        const float2 x = pair_of<T>(lo, i), y = pair_of<T>(hi, i);
-        ss = fmaf(x.x, x.x, fmaf(x.y, x.y, fmaf(y.x, y.x, fmaf(y.y, y.y, ss))));
+        const uint64_t x = pair_of<T>(lo, i), y = pair_of<T>(hi, i);
+        ss2 = ptx::fma2(x, x, ptx::fma2(y, y, ss2));
     }
+    float ss, other;
+    ptx::unpack2(ss2, ss, other);
+    ss += other;
     for (int s = 0; s < shift; ++s) ss += __shfl_xor_sync(0xffffffffu, ss, 1 << s);
-    return 1.f / sqrtf(ss / (float)D + eps);
+    return rsqrtf(fmaf(ss, 1.f / (float)D, eps));
 }
 
-// (cos, sin) of a token's D/2 angles in shared memory.  NORM: as floats, eight to 80 bytes, so that the lanes of a head start in
-// different banks; else as the rotation of a stored number wants them.
+// (cos, sin) of a token's D/2 angles in shared memory.  NORM: as floats, (cos, cos, sin, sin) of two channels, the four of eight channels to
+// 80 bytes, so that the lanes of a head start in different banks; else as the rotation of a stored number wants them.
 template <typename T, bool NORM> struct TokenAngles;
 template <typename T> struct TokenAngles<T, true> {
-    float2 at[80];
-    static __device__ __forceinline__ int place(int j) { return (j >> 3) * 10 + (j & 7); }
-    __device__ __forceinline__ void put(int j, const double2& cs) { at[place(j)] = make_float2((float)cs.x, (float)cs.y); }
+    float4 at[40];
+    static __device__ __forceinline__ int place(int pair) { return pair + (pair >> 2); }
+    __device__ __forceinline__ void put(int j, const double2& cs)
+    {
+        float* to = reinterpret_cast<float*>(at + place(j >> 1)) + (j & 1);
+        to[0] = (float)cs.x;
+        to[2] = (float)cs.y;
+    }
 };
 template <typename T> struct TokenAngles<T, false> {
     typename Rotation<T>::Angle at[Rotation<T>::kAngles];
     __device__ __forceinline__ void put(int j, const double2& cs) { Rotation<T>::put(at, j, cs); }
 };
 
-// A pair of vectors of a head, normed (all lanes of the warp call this) and turned; vector k of the half.  (Elements are taken out of the
-// vectors two at a time, and weights come late: with both as floats in registers the kernel needed 80 of them, and 3136 tokens took 27 us.)
+// Channels 2 i, 2 i + 1 of a head's vectors lo, hi (vector k of the half), times inv and the weights (if any: w0, w1), turned.
 template <typename T>
-__device__ __forceinline__ void norm_turn(const TokenAngles<T, true>& angles, int k, int shift, int D, float eps, const T* weight, const uint4& lo, const uint4& hi,
-                                          uint4& out_lo, uint4& out_hi)
+__device__ __forceinline__ void norm_turn_pair(const TokenAngles<T, true>& angles, int k, int i, float inv, bool weighted, const uint4& w0, const uint4& w1,
+                                               const uint4& lo, const uint4& hi, uint64_t& out_lo, uint64_t& out_hi)
+{
+    const uint64_t inv2 = ptx::pack2(inv, inv);
+    uint64_t x = ptx::mul2(pair_of<T>(lo, i), inv2), y = ptx::mul2(pair_of<T>(hi, i), inv2);
+    if (weighted) {
+        x = ptx::mul2(x, pair_of<T>(w0, i));
+        y = ptx::mul2(y, pair_of<T>(w1, i));
+    }
+    const float4 cs = angles.at[TokenAngles<T, true>::place(k * (VecTraits<T>::kVec / 2) + i)];
+    const uint64_t c = ptx::pack2(cs.x, cs.y), s = ptx::pack2(cs.z, cs.w), minus = ptx::pack2(-cs.z, -cs.w);
+    out_lo = ptx::fma2(x, c, ptx::mul2(y, minus));
+    out_hi = ptx::fma2(y, c, ptx::mul2(x, s));
+}
+
+// The heads of a token, by the lanes of one or several warps: work items it, it + step, ... of its items (pairs of vectors of query heads, of key
+// heads from q_items on, vectors of value heads from qk_items on; step is a multiple of 32, so a lane's place k in a head stays).  prepare() fills
+// the angles, while the first item's vectors are on their way, and returns the token's row in the cache; the next item's are requested
+// before an item is worked on.  All lanes of the warp call this.
+template <typename T, bool NORM, typename F>
+__device__ __forceinline__ void token_heads(const RopeArgs& a, const NormArgs& nrm, const TokenAngles<T, NORM>& angles, int tok, int it, int step, int q_items,
+                                            int qk_items, int items, long kv_rows, F&& prepare)
 {
     constexpr int V = VecTraits<T>::kVec;
-    uint4 w0 = make_uint4(0u, 0u, 0u, 0u), w1 = w0;
-    if (weight) {
-        w0 = *reinterpret_cast<const uint4*>(weight + k * V);
-        w1 = *reinterpret_cast<const uint4*>(weight + k * V + D / 2);
-    }
-    const float inv = norm_factor<T>(lo, hi, shift, D, eps);
-    const float4* a = reinterpret_cast<const float4*>(angles.at + TokenAngles<T, true>::place(k * V));
-#pragma unroll
-    for (int i = 0; i < V / 2; ++i) {
-        float2 x = pair_of<T>(lo, i), y = pair_of<T>(hi, i);
-        x.x *= inv; x.y *= inv; y.x *= inv; y.y *= inv;
-        if (weight) {
-            const float2 u = pair_of<T>(w0, i), v = pair_of<T>(w1, i);
-            x.x *= u.x; x.y *= u.y; y.x *= v.x; y.y *= v.y;
+    const int D = a.D, half = D / 2, vph = a.vph_shift, k = it & ((1 << vph) - 1), lane = threadIdx.x & 31;
+    const T* q = (const T*)a.q_new + tok * a.q_stride + k * V;
+    const T* kk = (const T*)a.k_new + tok * a.k_stride + k * V;
+    const T* v = (const T*)a.v_new + tok * a.v_stride;
+    auto load = [&](int i, uint4& r0, uint4& r1) {
+        r0 = r1 = make_uint4(0u, 0u, 0u, 0u);
+        if (i < qk_items) {
+            const T* src = (i < q_items ? q : kk) + ((i < q_items ? i : i - q_items) >> vph) * D;
+            r0 = *reinterpret_cast<const uint4*>(src);
+            r1 = *reinterpret_cast<const uint4*>(src + half);
+        } else if (i < items) {
+            r0 = *reinterpret_cast<const uint4*>(v + (i - qk_items) * V);
         }
-        const float4 cs = a[i];
-        set_pair<T>(out_lo, i, fmaf(x.x, cs.x, -(y.x * cs.y)), fmaf(x.y, cs.z, -(y.y * cs.w)));
-        set_pair<T>(out_hi, i, fmaf(y.x, cs.x, x.x * cs.y), fmaf(y.y, cs.z, x.y * cs.w));
+    };
+    uint4 n0, n1, w0 = make_uint4(0u, 0u, 0u, 0u), w1 = w0;
+    load(it, n0, n1);
+    const T* held = nullptr;                       // whose weights w0, w1 are
+    const long row = prepare();
+    T* q_rot = (T*)a.q_rot + (long)tok * a.G * D + k * V;
+    T* k_to = (T*)a.k_cache + row * D + k * V;
+    T* v_to = (T*)a.v_cache + row * D;
+#pragma unroll 1
+    for (; it - lane < items; it += step) {
+        const uint4 r0 = n0, r1 = n1;
+        load(it + step, n0, n1);                   // (two ahead: 16.0 us for 3136 tokens, one 15.0)
+        if (it - lane < qk_items) {                // (some lane of the warp)
+            const bool is_q = it < q_items;
+            uint4 y0, y1;
+            if constexpr (NORM) {
+                const T* weight = (const T*)(is_q ? nrm.q_weight : nrm.k_weight);
+                if (weight != held) {
+                    held = weight;
+                    if (weight) {
+                        w0 = *reinterpret_cast<const uint4*>(weight + k * V);
+                        w1 = *reinterpret_cast<const uint4*>(weight + k * V + half);
+                    }
+                }
+                const float inv = norm_factor<T>(r0, r1, vph, D, nrm.eps);
+#pragma unroll
+                for (int i = 0; i < V / 2; ++i) {
+                    uint64_t lo, hi;
+                    norm_turn_pair<T>(angles, k, i, inv, weight != nullptr, w0, w1, r0, r1, lo, hi);
+                    set_pair<T>(y0, i, lo);
+                    set_pair<T>(y1, i, hi);
+                }
+            } else {
+                Rotation<T>::turn(angles.at, k, r0, r1, y0, y1);
+            }
+            if (it < qk_items) {
+                const int h = (is_q ? it : it - q_items) >> vph, g = (int)fast_div((uint32_t)h, a.div_g);
+                T* dst = is_q ? q_rot + ((long)g * (a.num_new - 1) * a.G + h) * D : k_to + h * kv_rows * D;
+                *reinterpret_cast<uint4*>(dst) = y0;
+                *reinterpret_cast<uint4*>(dst + half) = y1;
+            }
+        }
+        if (it >= qk_items && it < items) {
+            const int e = it - qk_items;
+            *reinterpret_cast<uint4*>(v_to + (e >> (vph + 1)) * kv_rows * D + (e & ((2 << vph) - 1)) * V) = r0;
+        }
     }
 }
 
-// One block per new token (gridDim.y: and part of its work items); PAGED: then one per episode that clears the value slots behind
-// its last token.
-template <typename T, bool PAGED, typename LensT>
-__global__ void __launch_bounds__(kRopeThreadsMax, 3)
-norm_append_kernel(const RopeArgs a, const NormArgs nrm, const __grid_constant__ LensT lens)
+// Fills a token's angles by the lanes of a warp; omega: of angle lane and, D = 128, lane + 32 (without a table).
+template <bool TABLE, typename Angles>
+__device__ __forceinline__ void fill_angles(Angles& s, const RopeArgs& a, int pos, const double (&omega)[2])
+{
+    const int half = a.D / 2, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int j = lane + 32 * i;
+        if (j < half) s.put(j, TABLE ? a.table[(long)(pos - a.table_first) * half + j] : rope_cos_sin_at(pos, omega[i]));
+    }
+    __syncwarp();
+}
+template <bool TABLE>
+__device__ __forceinline__ void own_omegas(const RopeArgs& a, double (&omega)[2])
+{
+    const int lane = threadIdx.x & 31;
+    omega[0] = omega[1] = 0.0;
+    if (!TABLE) {
+        omega[0] = rope_omega(lane, a.D, a.log2_theta);
+        if (a.D > 64) omega[1] = rope_omega(lane + 32, a.D, a.log2_theta);
+    }
+}
+
+// token_warps warps per new token, each with every token_warps-th 32 of its items; PAGED: then one per episode and head that clears the value
+// slots behind the episode's last token.
+template <typename T, bool PAGED, bool TABLE, typename LensT>
+__global__ void __launch_bounds__(32 * kNormWarps, kNormBlocks)
+norm_append_kernel(const RopeArgs a, const NormArgs nrm, int token_warps, FastDiv div_warps, const __grid_constant__ LensT lens)
 {
     constexpr int V = VecTraits<T>::kVec;
-    __shared__ __align__(16) TokenAngles<T, true> s_angles;
-    const int D = a.D, half = D / 2, vph = a.vph_shift;
-    int b = 0;
-    if (PAGED && (int)blockIdx.x >= a.num_new) {
-        b = blockIdx.x - a.num_new;
-        const int len = lens.cache_len[b] + lens.new_off[b + 1] - lens.new_off[b], used = len & (a.page_size - 1);
+    __shared__ __align__(16) TokenAngles<T, true> s_angles[kNormWarps];
+    const int D = a.D, vph = a.vph_shift, wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int w = blockIdx.x * kNormWarps + wid, tok = (int)fast_div((uint32_t)w, div_warps), part = w - tok * token_warps;
+    if (tok >= a.num_new) {
+        const int at = w - a.num_new * token_warps, b = at / a.Hkv, g = at - b * a.Hkv;
         ptx::grid_dependency_wait();
         ptx::grid_launch_dependents();
+        if (!PAGED || b >= a.batch) return;
+        const int len = lens.cache_len[b] + lens.new_off[b + 1] - lens.new_off[b], used = len & (a.page_size - 1);
         if (lens.new_off[b + 1] == lens.new_off[b] || used == 0) return;
-        const long row = (long)a.page_table[(long)b * a.max_pages + (len >> a.page_shift)] * a.Hkv * a.page_size + used;
-        for (int g = blockIdx.y; g < a.Hkv; g += gridDim.y) {
-            uint4* dst = reinterpret_cast<uint4*>((T*)a.v_cache + (row + (long)g * a.page_size) * D);
-            for (int it = threadIdx.x; it < (a.page_size - used) * (D / V); it += blockDim.x) dst[it] = make_uint4(0u, 0u, 0u, 0u);
-        }
+        const long row = ((long)a.page_table[(long)b * a.max_pages + (len >> a.page_shift)] * a.Hkv + g) * a.page_size + used;
+        uint4* dst = reinterpret_cast<uint4*>((T*)a.v_cache + row * D);
+        for (int it = lane; it < (a.page_size - used) * (D / V); it += 32) dst[it] = make_uint4(0u, 0u, 0u, 0u);
         return;
     }
-    const int tok = blockIdx.x;
-    if (PAGED) {
-        int hi = a.batch;                         // largest b with new_off[b] <= tok
-        while (hi - b > 1) {
-            const int mid = (b + hi) >> 1;
-            if (lens.new_off[mid] <= tok) b = mid; else hi = mid;
-        }
-    }
-    const int pos = PAGED ? lens.cache_len[b] + tok - lens.new_off[b] : a.cache_len + tok;
-    // without a table: the thread's frequency, ahead of the wait (launch parameters only)
-    const double omega = !a.table && (int)threadIdx.x < half ? rope_omega(threadIdx.x, D, a.log2_theta) : 0.0;
+    double omega[2];
+    own_omegas<TABLE>(a, omega);
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
-
-    const int q_items = a.Hq << vph, qk_items = q_items + (a.Hkv << vph), items = qk_items + (a.Hkv << (vph + 1)), step = gridDim.y * blockDim.x;
-    const int k = (int)threadIdx.x & ((1 << vph) - 1);            // (blocks are whole warps, so a thread's place in a head stays)
-    auto load = [&](int it, uint4& r0, uint4& r1) {               // a pair of vectors of a query or key head, or a vector of a value head
-        r0 = r1 = make_uint4(0u, 0u, 0u, 0u);
-        if (it < qk_items) {
-            const bool is_q = it < q_items;
-            const T* src = (is_q ? (const T*)a.q_new + tok * a.q_stride : (const T*)a.k_new + tok * a.k_stride) + (long)((is_q ? it : it - q_items) >> vph) * D + k * V;
-            r0 = *reinterpret_cast<const uint4*>(src);
-            r1 = *reinterpret_cast<const uint4*>(src + half);
-        } else if (it < items) {
-            r0 = *reinterpret_cast<const uint4*>((const T*)a.v_new + tok * a.v_stride + (long)(it - qk_items) * V);
-        }
-    };
-    uint4 r0, r1;
-    int it = blockIdx.y * blockDim.x + threadIdx.x;
-    load(it, r0, r1);                              // in flight while the angles arrive
-    if ((int)threadIdx.x < half) s_angles.put(threadIdx.x, a.table ? a.table[(long)(pos - a.table_first) * half + threadIdx.x] : rope_cos_sin_at(pos, omega));
-    const long row = PAGED ? (long)a.page_table[(long)b * a.max_pages + (pos >> a.page_shift)] * a.Hkv * a.page_size + (pos & (a.page_size - 1)) : pos;
-    const long kv_rows = PAGED ? a.page_size : a.cache_cap;
-    __syncthreads();
-    for (;;) {
-        uint4 y0 = r0, y1 = r1;
-        const bool is_q = it < q_items;
-        if (it - (int)(threadIdx.x & 31) < qk_items)              // (some lane of the warp)
-            norm_turn<T>(s_angles, k, vph, D, nrm.eps, (const T*)(is_q ? nrm.q_weight : nrm.k_weight), r0, r1, y0, y1);
-        if (it < qk_items) {
-            const int h = (is_q ? it : it - q_items) >> vph;
-            T* dst;
-            if (is_q) {
-                const int g = (int)fast_div((uint32_t)h, a.div_g);
-                dst = (T*)a.q_rot + ((long)g * a.num_new * a.G + (long)tok * a.G + (h - g * a.G)) * D;
-            } else {
-                dst = (T*)a.k_cache + (h * kv_rows + row) * D;
+    const int q_items = a.Hq << vph, qk_items = q_items + (a.Hkv << vph), items = qk_items + (a.Hkv << (vph + 1));
+    token_heads<T, true>(a, nrm, s_angles[wid], tok, 32 * part + lane, 32 * token_warps, q_items, qk_items, items, PAGED ? a.page_size : a.cache_cap, [&]() -> long {
+        int b = 0;
+        if (PAGED) {
+            int hi = a.batch;                     // largest b with new_off[b] <= tok
+            while (hi - b > 1) {
+                const int mid = (b + hi) >> 1;
+                if (lens.new_off[mid] <= tok) b = mid; else hi = mid;
             }
-            *reinterpret_cast<uint4*>(dst + k * V) = y0;
-            *reinterpret_cast<uint4*>(dst + k * V + half) = y1;
-        } else if (it < items) {
-            const int e = it - qk_items;
-            *reinterpret_cast<uint4*>((T*)a.v_cache + ((e >> (vph + 1)) * kv_rows + row) * D + (e & ((2 << vph) - 1)) * V) = r0;
         }
-        it += step;
-        if (it - (int)(threadIdx.x & 31) >= items) break;
-        load(it, r0, r1);
-    }
+        const int pos = PAGED ? lens.cache_len[b] + tok - lens.new_off[b] : a.cache_len + tok;
+        const long row = PAGED ? (long)a.page_table[(long)b * a.max_pages + (pos >> a.page_shift)] * a.Hkv * a.page_size + (pos & (a.page_size - 1)) : pos;
+        fill_angles<TABLE>(s_angles[wid], a, pos, omega);
+        return row;
+    });
 }
 
 }  // namespace evln
