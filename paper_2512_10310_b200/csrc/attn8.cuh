@@ -20,7 +20,7 @@
 // unit by unit (unit: episode, kv head).  Nothing is shared between key groups until all are done: then the
 // results of neighbouring runs that ended in the same unit are joined in the shared memory that the rings leave.  (Stages dealt
 // to the warps in turn, which joins all of them at the end of every unit, took 45 us for 16 ragged episodes of a token, runs 38.)
-// Runs are equally long, KG of them per SM; a unit that the runs cut across blocks leaves normalised parts, which merge8_kernel
+// Runs are equally long, KG of them per SM; a unit that the runs cut across blocks leaves parts, which merge8_kernel
 // joins.  The lanes of a warp look 32 stages ahead for page numbers and scales (a lane each).
 // A row's reference m follows its maximum only when that is 2^8 above it, so outputs are rarely scaled anew.
 #pragma once
@@ -35,7 +35,7 @@
 namespace evln {
 
 constexpr int kA8Keys = 32, kA8StageBytes = 2 * kA8Keys * 128;
-constexpr int kA8OStride = 136;                       // floats between rows of the joint's buffers (neighbouring rows start 8 banks apart)
+constexpr int kA8OStride = 132;                       // floats between rows of the joint's buffers (every second one starts 8 banks on)
 constexpr float kA8Headroom = 8.f, kA8Lift = 6.f;     // p' <= 2^(headroom + lift), below the largest half
 constexpr float kA8LeastRatio = -40.f;                // log2 of the smallest value-scale ratio that is told apart (halves end at -24 - lift)
 
@@ -44,11 +44,10 @@ struct Attn8Plan {
     // Twelve warps, three a scheduler that hide each other's chains.  (Eight of 255 registers with 32 rows each take 5 to 10 % less for large batches of
     // 17 to 64 rows, 16 episodes of 8000 keys 86 us and 95, but more where latency counts, one of 4096 keys 14.5 and 12.5.)
     static constexpr int kWarps = 12, kThreads = 32 * kWarps;
-    // (8 rows need no more than 144 registers, which leaves the SM room for blocks of the merge kernel)
-    static constexpr int kRegs = NQ == 1 ? 144 : 168;
+    static constexpr int kRegs = 168;
     static constexpr int kWarpRows = 8 * NQ, kRows = kWarpRows * RG;
     static constexpr int kKeyGroups = kWarps / RG;
-    static constexpr int kStatBytes = kWarps * kWarpRows * 8 + 64;             // references and sums, the units that the runs ended in
+    static constexpr int kStatBytes = kWarps * kWarpRows * 8 + 128;            // references and sums; value scales of the runs, the units that they ended in
     static constexpr int kBarBytes = 512;
     static constexpr int kRest = kStatBytes + kBarBytes + 1024;
     static constexpr int kFit = (227 * 1024 - kRest) / kA8StageBytes / kKeyGroups;
@@ -58,7 +57,7 @@ struct Attn8Plan {
     static constexpr int kBytes = kRing + kRest;
     static_assert(kSlots >= 2, "a stage in flight beside the one that is read");
     static_assert(16 * kKeyGroups * kSlots + 8 <= kBarBytes, "barriers");
-    static_assert(kWarps * kWarpRows * kA8OStride * 4 <= kRing, "the joint's buffers");
+    static_assert(kRows * kA8OStride * 4 <= kSlots * kA8StageBytes, "the joint's buffers, each in its own ring");
     static_assert(NQ <= 2, "a 16-row tile of queries in a warp's registers");
     static_assert(kBarOff % 8 == 0 && kBytes <= 227 * 1024, "shared memory of a block");
 };
@@ -71,7 +70,7 @@ struct Attn8Args {
     __nv_bfloat16* out;              // [tokens, Hq, 128]
     float* lse_out;                  // [tokens, Hq] or null
     float* o_part;                   // [2 * runs, rows of a block, 128]
-    float* lse_part;                 // [2 * runs, rows of a block], log2
+    float2* ml_part;                 // [2 * runs, rows of a block]: reference (log2) and sum
     int* status;
     int Hkv, G, rows, batch, max_pages;
     int run, total;                  // stages of a run, of the batch
@@ -130,9 +129,9 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
-    float* s_m = reinterpret_cast<float*>(smem_gen + Plan::kStatOff);              // [warp][WROWS]
-    float* s_l = s_m + Plan::kWarps * WROWS;
-    int* s_unit = reinterpret_cast<int*>(s_l + Plan::kWarps * WROWS);              // [KG] first stage of the unit that the run ended in, -1: nothing left
+    float2* s_ml = reinterpret_cast<float2*>(smem_gen + Plan::kStatOff);           // [KG][ROWS]
+    float* s_scale = reinterpret_cast<float*>(s_ml + KG * ROWS);                   // [KG]
+    int* s_unit = reinterpret_cast<int*>(s_scale + KG);                            // [KG] first stage of the unit that the run ended in, -1: nothing left
     volatile int* s_abort = reinterpret_cast<volatile int*>(smem_gen + Plan::kBarOff + 16 * KG * SLOTS);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = lane & 3, lrow = lane >> 2;
@@ -389,72 +388,54 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         if (!left) {
 #pragma unroll
             for (int q = 0; q < NQ; ++q) {
-                const float by_row = l[q] == 0.f ? 0.f : ref_scale * exp2_int(-(int)kA8Lift) / l[q], lse_row = l[q] == 0.f ? -INFINITY : m[q] + log2f(l[q]);
+                const float value = ref_scale * exp2_int(-(int)kA8Lift), by_row = !whole ? value : l[q] == 0.f ? 0.f : value / l[q];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float by = __shfl_sync(0xffffffffu, by_row, 8 * quad + 4 * e), lse2 = __shfl_sync(0xffffffffu, lse_row, 8 * quad + 4 * e);
+                    const int from = 8 * quad + 4 * e;
+                    const float by = __shfl_sync(0xffffffffu, by_row, from), mr = __shfl_sync(0xffffffffu, m[q], from), lr = __shfl_sync(0xffffffffu, l[q], from);
                     const int r = q * 8 + 2 * quad + e;
                     if (row0 + r >= rows_here) continue;
                     if (whole) {
                         const long at = out_row8(a, lens, u, row0 + r);
 #pragma unroll
                         for (int c = 0; c < 8; ++c) reinterpret_cast<uint32_t*>(a.out + at * 128)[8 * c + lrow] = ptx::pack_bf16x2(o[q][c][e] * by, o[q][c][2 + e] * by);
-                        if (a.lse_out && lrow == 0) a.lse_out[at] = lse2 * kLn2;
+                        if (a.lse_out && lrow == 0) a.lse_out[at] = (mr + log2f(lr)) * kLn2;
                     } else {
                         const long at = 2L * run * ROWS + row0 + r;
 #pragma unroll
                         for (int c = 0; c < 8; ++c) reinterpret_cast<float2*>(a.o_part + at * 128)[8 * c + lrow] = make_float2(o[q][c][e] * by, o[q][c][2 + e] * by);
-                        if (lrow == 0) a.lse_part[at] = lse2;
+                        if (lrow == 0) a.ml_part[at] = make_float2(mr, lr);
                     }
                 }
             }
         }
     }
 
-    // ---- the joint: runs of the block that ended in the same unit ----
-    if (rg == 0 && lane == 0) s_unit[kg] = left ? u.first : -1;
-    if (left && quad == 0) {
+    // ---- the joint: runs of the block that ended in the same unit; a group's rows go to its own ring, whose loads have all been waited for ----
+    // (Code that runs once costs its fetch, some 0.1 us for each 100 instructions: hence one barrier and rolled loops.)
+    if (RG > 1) asm volatile("bar.sync %0, %1;" :: "r"(1 + kg), "n"(32 * RG) : "memory");
+    else __syncwarp();
+    if (rg == 0 && lane == 0) {
+        s_unit[kg] = left ? u.first : -1;
+        s_scale[kg] = ref_scale * exp2_int(-(int)kA8Lift);
+    }
+    if (left) {
+        float* to = reinterpret_cast<float*>(smem_gen + kg * SLOTS * kA8StageBytes) + (rg * WROWS + 2 * quad) * kA8OStride + 2 * lrow;
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-            s_m[warp * WROWS + q * 8 + lrow] = m[q];
-            s_l[warp * WROWS + q * 8 + lrow] = l[q];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int c = 0; c < 8; ++c) *reinterpret_cast<float2*>(to + (q * 8 + e) * kA8OStride + 16 * c) = make_float2(o[q][c][e], o[q][c][2 + e]);
+            if (quad == 0) s_ml[kg * ROWS + rg * WROWS + q * 8 + lrow] = make_float2(m[q], l[q]);
         }
     }
-    __syncthreads();                                   // (every load has been waited for: the rings are free)
+    __syncthreads();
     if (*s_abort) {
         const long long t0 = clock64();                // loads in flight land before the block may leave
         while (clock64() - t0 < 400000) { }
         return;
     }
-    float* s_o = reinterpret_cast<float*>(smem_gen);   // [warp][WROWS][kA8OStride]
-    float top[NQ];
-    if (left) {
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-            top[q] = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < KG; ++k)
-                if (s_unit[k] == u.first) top[q] = fmaxf(top[q], s_m[(k * RG + rg) * WROWS + q * 8 + lrow]);
-            const float w = m[q] == -INFINITY ? 0.f : ptx::ex2(m[q] - top[q]), by_row = w * ref_scale * exp2_int(-(int)kA8Lift);
-            l[q] = l[q] == 0.f ? 0.f : l[q] * w;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float by = __shfl_sync(0xffffffffu, by_row, 8 * quad + 4 * e);
-                float2* to = reinterpret_cast<float2*>(s_o + (warp * WROWS + q * 8 + 2 * quad + e) * kA8OStride) + lrow;
-#pragma unroll
-                for (int c = 0; c < 8; ++c) to[8 * c] = make_float2(o[q][c][e] * by, o[q][c][2 + e] * by);
-            }
-        }
-    }
-    __syncthreads();                                   // (the references are read)
-    if (left && quad == 0) {
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-            s_m[warp * WROWS + q * 8 + lrow] = top[q];
-            s_l[warp * WROWS + q * 8 + lrow] = l[q];
-        }
-    }
-    __syncthreads();
     for (int k0 = 0; k0 < KG;) {
         const int at_unit = s_unit[k0];
         int k1 = k0 + 1;
@@ -464,28 +445,34 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             const int first_run = blockIdx.x * KG + k0, ends = min(a.total, (blockIdx.x * KG + k1) * a.run);
             const bool whole = first_run * a.run <= w.first && ends == w.first + w.stages;
             const int rows_here = w.n * a.G;
-            for (int r = tid >> 5; r < rows_here; r += Plan::kWarps) {               // a warp per row, four channels a lane
-                const int at0 = (k0 * RG + r / WROWS) * WROWS + r % WROWS;
-                float sum = 0.f;
-                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+            for (int r = warp; r < rows_here; r += Plan::kWarps) {                   // a warp per row: a lane per run, then four channels a lane
+                const int k = k0 + lane;
+                const float2 ml = k < k1 ? s_ml[k * ROWS + r] : make_float2(-INFINITY, 0.f);
+                float top = ml.x;
 #pragma unroll
-                for (int k = 0; k < KG; ++k) {
-                    if (k0 + k >= k1) continue;
-                    const int at = at0 + k * RG * WROWS;
-                    const float4 y = *reinterpret_cast<const float4*>(s_o + at * kA8OStride + 4 * lane);
-                    sum += s_l[at];
-                    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+                float by = ml.x == -INFINITY ? 0.f : ptx::ex2(ml.x - top), sum = ml.y * by;
+#pragma unroll
+                for (int s = 16; s > 0; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+                if (k < k1) by *= s_scale[k];
+                if (whole) by = sum == 0.f ? 0.f : by / sum;
+                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                const float* from = reinterpret_cast<const float*>(smem_gen + k0 * SLOTS * kA8StageBytes) + r * kA8OStride + 4 * lane;
+#pragma unroll 3
+                for (int j = 0; j < k1 - k0; ++j, from += SLOTS * (kA8StageBytes / 4)) {
+                    const float4 y = *reinterpret_cast<const float4*>(from);
+                    const float f = __shfl_sync(0xffffffffu, by, j);
+                    x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
                 }
-                const float by = sum == 0.f ? 0.f : 1.f / sum, lse2 = sum == 0.f ? -INFINITY : s_m[at0] + log2f(sum);
-                x.x *= by; x.y *= by; x.z *= by; x.w *= by;
                 if (whole) {
                     const long at = out_row8(a, lens, w, r);
                     reinterpret_cast<uint2*>(a.out + at * 128)[lane] = make_uint2(ptx::pack_bf16x2(x.x, x.y), ptx::pack_bf16x2(x.z, x.w));
-                    if (a.lse_out && lane == 0) a.lse_out[at] = lse2 * kLn2;
+                    if (a.lse_out && lane == 0) a.lse_out[at] = (top + log2f(sum)) * kLn2;
                 } else {
                     const long at = (2L * first_run + 1) * ROWS + r;
                     reinterpret_cast<float4*>(a.o_part + at * 128)[lane] = x;
-                    if (lane == 0) a.lse_part[at] = lse2;
+                    if (lane == 0) a.ml_part[at] = make_float2(top, sum);
                 }
             }
         }
@@ -502,15 +489,19 @@ struct MergeList {
 };
 
 // Joins the parts of the units that the runs cut: what each block's runs that end in the unit left jointly, and what a run left that goes on
-// behind its end.  Blocks (x, y): units as in MergeList, rows y, y + gridDim.y, ...; the four warps share a row's parts.
+// behind its end.  Blocks (x, y): units as in MergeList, rows y, y + gridDim.y, ...; the warps share a row's parts, each with up to kMergeAhead
+// of them in flight beside the references, before it is known what they weigh.
 // Blocks without such a unit leave at once (the first one does not: the next kernel in the stream waits for this grid, which
 // therefore must not end before the attention kernel has), so the others are on the SMs, and know what to read, when the parts are there.
+constexpr int kMergeAhead = 5;                         // (64 rows of one episode of 20656 keys: 25.5 us in all, with 3 26.4)
+template <int ROWS> constexpr int kMergeWarps = ROWS >= 32 ? 8 : 4;            // (8 and 16 rows: few parts, many units)
 template <int ROWS, int KG>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(32 * kMergeWarps<ROWS>)
 merge8_kernel(const Attn8Args a, const __grid_constant__ BatchLens lens, const __grid_constant__ MergeList list)
 {
-    __shared__ float4 s_x[4][32];
-    __shared__ float s_sum[4];
+    constexpr int WARPS = kMergeWarps<ROWS>;
+    __shared__ float4 s_x[WARPS][32];
+    __shared__ float s_sum[WARPS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Unit8 u;
     int u1, ra, rb;
@@ -542,32 +533,55 @@ merge8_kernel(const Attn8Args a, const __grid_constant__ BatchLens lens, const _
         const int b0 = ra / KG, joints = (on ? rb - 1 : rb) / KG - b0 + 1, parts = joints + (on ? 1 : 0);
         auto row_of = [&](int p, int r) -> long { return (p < joints ? 2L * max(ra, (b0 + p) * KG) + 1 : 2L * rb) * ROWS + r; };
         for (int r = blockIdx.y; r < u.n * a.G; r += gridDim.y) {
+            float4 y[kMergeAhead];
+            float2 ml[kMergeAhead];
+            auto fetch = [&](int p0) {
+#pragma unroll
+                for (int i = 0; i < kMergeAhead; ++i) {
+                    const int p = p0 + WARPS * i;
+                    ml[i] = make_float2(-INFINITY, 0.f);
+                    if (p < parts) {
+                        const long at = row_of(p, r);
+                        y[i] = reinterpret_cast<const float4*>(a.o_part + at * 128)[lane];
+                        ml[i] = a.ml_part[at];
+                    }
+                }
+            };
+            fetch(warp);
             float top = -INFINITY, sum = 0.f;
-            for (int p = lane; p < parts; p += 32) top = fmaxf(top, a.lse_part[row_of(p, r)]);
+            for (int p = lane; p < parts; p += 32) top = fmaxf(top, a.ml_part[row_of(p, r)].x);
 #pragma unroll
             for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-            for (int p = warp; p < parts; p += 4) {
-                const long at = row_of(p, r);
-                const float4 y = reinterpret_cast<const float4*>(a.o_part + at * 128)[lane];
-                const float w = ptx::ex2(a.lse_part[at] - top);      // 0: no key of the row in this part
-                sum += w;
-                x.x = fmaf(y.x, w, x.x); x.y = fmaf(y.y, w, x.y); x.z = fmaf(y.z, w, x.z); x.w = fmaf(y.w, w, x.w);
+#pragma unroll 1
+            for (int p0 = warp;;) {
+#pragma unroll
+                for (int i = 0; i < kMergeAhead; ++i) {
+                    if (p0 + WARPS * i >= parts) break;
+                    const float w = ml[i].x == -INFINITY ? 0.f : ptx::ex2(ml[i].x - top);      // -inf: no key of the row in this part
+                    sum = fmaf(ml[i].y, w, sum);
+                    x.x = fmaf(y[i].x, w, x.x); x.y = fmaf(y[i].y, w, x.y); x.z = fmaf(y[i].z, w, x.z); x.w = fmaf(y[i].w, w, x.w);
+                }
+                p0 += WARPS * kMergeAhead;
+                if (p0 >= parts) break;
+                fetch(p0);
             }
             s_x[warp][lane] = x;
             if (lane == 0) s_sum[warp] = sum;
             __syncthreads();
-            if (warp == 0) {
-                for (int w = 1; w < 4; ++w) {
-                    const float4 y = s_x[w][lane];
-                    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+            if (threadIdx.x < 64) {                                  // a pair of channels a thread
+                float2 z = make_float2(0.f, 0.f);
+                sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < WARPS; ++w) {
+                    const float2 part = reinterpret_cast<const float2*>(s_x[w])[threadIdx.x];
+                    z.x += part.x; z.y += part.y;
                     sum += s_sum[w];
                 }
                 const float by = 1.f / sum;
                 const long at = out_row8(a, lens, u, r);
-                reinterpret_cast<uint2*>(a.out + at * 128)[lane] = make_uint2(ptx::pack_bf16x2(x.x * by, x.y * by), ptx::pack_bf16x2(x.z * by, x.w * by));
-                if (a.lse_out && lane == 0) a.lse_out[at] = (top + log2f(sum)) * kLn2;
+                reinterpret_cast<uint32_t*>(a.out + at * 128)[threadIdx.x] = ptx::pack_bf16x2(z.x * by, z.y * by);
+                if (a.lse_out && threadIdx.x == 0) a.lse_out[at] = (top + log2f(sum)) * kLn2;
             }
             __syncthreads();
         }

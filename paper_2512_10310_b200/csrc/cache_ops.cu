@@ -192,7 +192,7 @@ evlnStatus_t plan8(evlnHandle_t h, const evlnPagedParams* p, const int* lens, co
     return EVLN_OK;
 }
 
-size_t part_bytes8(const Plan8& pl) { return round_up((size_t)2 * pl.runs * pl.rows * (128 + 1) * sizeof(float), 256); }
+size_t part_bytes8(const Plan8& pl) { return round_up((size_t)2 * pl.runs * pl.rows * (128 + 2) * sizeof(float), 256); }
 
 // The paged call that serves the bf16 copy.
 evlnPagedParams copy_params(const evlnPagedParams* p, const Plan8& pl)
@@ -218,7 +218,7 @@ cudaError_t launch_attn8(const Plan8& pl, cudaStream_t st, const CUtensorMap& tm
         }
         const bool few = list.count <= kMergeUnits;
         if (!few) list.count = 0;
-        e = launch_pdl(merge8_kernel<Plan::kRows, Plan::kKeyGroups>, dim3(few ? list.count : pl.blocks, few || pl.most < 16 ? pl.most : 16), dim3(128), 0, st, a, bl, list);
+        e = launch_pdl(merge8_kernel<Plan::kRows, Plan::kKeyGroups>, dim3(few ? list.count : pl.blocks, few || pl.most < 16 ? pl.most : 16), dim3(32 * kMergeWarps<Plan::kRows>), 0, st, a, bl, list);
     }
     return e;
 }
@@ -394,7 +394,7 @@ evlnStatus_t evlnPaged8StepAttention(evlnHandle_t h, const evlnPagedParams* p, c
     a.page_table = d_page_table;
     a.out = (__nv_bfloat16*)out; a.lse_out = lse_out;
     a.o_part = (float*)workspace;
-    a.lse_part = a.o_part + (size_t)2 * pl.runs * pl.rows * 128;
+    a.ml_part = (float2*)(a.o_part + (size_t)2 * pl.runs * pl.rows * 128);
     a.status = h->d_status;
     a.Hkv = hkv; a.G = G; a.rows = total * G; a.batch = p->batch; a.max_pages = p->max_pages_per_seq;
     a.run = pl.run; a.total = pl.total;
