@@ -36,8 +36,9 @@ namespace evln {
 
 constexpr int kA8Keys = 32, kA8StageBytes = 2 * kA8Keys * 128;
 constexpr int kA8OStride = 132;                       // floats between rows of the joint's buffers (every second one starts 8 banks on)
-constexpr float kA8Headroom = 8.f, kA8Lift = 6.f;     // p' <= 2^(headroom + lift), below the largest half
-constexpr float kA8LeastRatio = -40.f;                // log2 of the smallest value-scale ratio that is told apart (halves end at -24 - lift)
+constexpr float kA8Headroom = 8.f;                    // p' <= 2^(headroom + lift), below the largest half
+constexpr int kA8Lift = 6;
+constexpr int kA8LeastRatio = -40;                    // log2 of the smallest value-scale ratio that is told apart (halves end at -24 - lift)
 
 template <int NQ, int RG>
 struct Attn8Plan {
@@ -237,7 +238,8 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     int i = 0, slot = 0;                               // the run's next stage
     uint32_t parity = 0;
     // o: transposed, [8-row tile][16 channels 16 c ..]: channels 16 c + 2 lrow (first two) and + 1, rows 2 quad and 2 quad + 1 of the tile; m, l: rows lrow
-    float o[NQ][8][4], m[NQ], l[NQ], ref_scale = 0.f;                  // ref_scale: the largest value scale so far
+    float o[NQ][8][4], m[NQ], l[NQ];
+    int ref = 0;                                       // the largest value scale so far, as the float's exponent field; 0: none
     bool left = false;                                 // the unit at hand goes to the joint
     while (i < mine) {
         if (i > 0) {
@@ -258,7 +260,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             m[q] = -INFINITY;
             l[q] = 0.f;
         }
-        ref_scale = 0.f;
+        ref = 0;
 
         for (; r0 + i < end; ++i) {
             if ((i & 31) == 0 && i > 0) {
@@ -290,10 +292,13 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                     }
                 }
                 // ---- softmax: references, probabilities, sums ----
-                const bool grew = vs > ref_scale;                     // uniform over the warp
-                const float shrink = grew ? ref_scale / vs : 1.f;
-                if (grew) ref_scale = vs;
-                const float ratio = fmaxf(log2f(vs / ref_scale), kA8LeastRatio) + kA8Lift, unlift = ptx::ex2(-ratio);
+                const int own = (int)(__float_as_uint(vs) >> 23);     // (a power of two; uniform over the warp)
+                const bool grew = own > ref;
+                const float shrink = !grew ? 1.f : own - ref > 100 ? 0.f : exp2_int(ref - own);
+                bool moved = grew && ref > 0;
+                if (grew) ref = own;
+                const int steps = max(own - ref, kA8LeastRatio) + kA8Lift;
+                const float ratio = (float)steps, unlift = exp2_int(-steps);
                 if (key0 + kA8Keys - 1 > u.L) {                       // keys that not every row sees
 #pragma unroll
                     for (int q = 0; q < NQ; ++q)
@@ -304,7 +309,6 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                                 if (key0 + 8 * t + 2 * quad + e > last[q]) sc[t][2 * q + e] = -INFINITY;
                 }
                 uint32_t p[NQ][2][2];                                 // the transposed product's operand: two k-steps of 16 keys
-                bool moved = grew && shrink > 0.f;
                 float keep[NQ];
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
@@ -388,7 +392,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         if (!left) {
 #pragma unroll
             for (int q = 0; q < NQ; ++q) {
-                const float value = ref_scale * exp2_int(-(int)kA8Lift), by_row = !whole ? value : l[q] == 0.f ? 0.f : value / l[q];
+                const float value = __uint_as_float((uint32_t)(ref - kA8Lift) << 23), by_row = !whole ? value : l[q] == 0.f ? 0.f : value / l[q];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int from = 8 * quad + 4 * e;
@@ -417,7 +421,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     else __syncwarp();
     if (rg == 0 && lane == 0) {
         s_unit[kg] = left ? u.first : -1;
-        s_scale[kg] = ref_scale * exp2_int(-(int)kA8Lift);
+        s_scale[kg] = __uint_as_float((uint32_t)(ref - kA8Lift) << 23);
     }
     if (left) {
         float* to = reinterpret_cast<float*>(smem_gen + kg * SLOTS * kA8StageBytes) + (rg * WROWS + 2 * quad) * kA8OStride + 2 * lrow;
@@ -436,38 +440,39 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         while (clock64() - t0 < 400000) { }
         return;
     }
+    const int unit_of = s_unit[lane < KG ? lane : KG - 1];
     for (int k0 = 0; k0 < KG;) {
-        const int at_unit = s_unit[k0];
-        int k1 = k0 + 1;
-        while (k1 < KG && s_unit[k1] == at_unit) ++k1;
+        const int at_unit = __shfl_sync(0xffffffffu, unit_of, k0);
+        const unsigned others = __ballot_sync(0xffffffffu, lane > k0 && lane < KG && unit_of != at_unit);
+        const int k1 = others ? __ffs(others) - 1 : KG;
         if (at_unit >= 0) {
             const Unit8 w = left && u.first == at_unit ? u : unit8_at(lens, a.batch, at_unit);
             const int first_run = blockIdx.x * KG + k0, ends = min(a.total, (blockIdx.x * KG + k1) * a.run);
             const bool whole = first_run * a.run <= w.first && ends == w.first + w.stages;
             const int rows_here = w.n * a.G;
 #pragma unroll 1
-            for (int r = warp; r < rows_here; r += Plan::kWarps) {                   // a warp per row: a lane per run, then four channels a lane
-                const int k = k0 + lane;
-                const float2 ml = k < k1 ? s_ml[k * ROWS + r] : make_float2(-INFINITY, 0.f);
-                float top = ml.x;
+            for (int r = warp; r < rows_here; r += Plan::kWarps) {                   // a warp per row, four channels a lane
+                float2 ml[KG];
+                float4 y[KG];
+                float top = -INFINITY, sum = 0.f;
 #pragma unroll
-                for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-                float by = ml.x == -INFINITY ? 0.f : ptx::ex2(ml.x - top), sum = ml.y * by;
-#pragma unroll
-                for (int s = 16; s > 0; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
-                if (k < k1) by *= s_scale[k];
-                if (whole) by = sum == 0.f ? 0.f : by / sum;
+                for (int k = 0; k < KG; ++k) {
+                    const bool in = k >= k0 && k < k1;
+                    ml[k] = in ? s_ml[k * ROWS + r] : make_float2(-INFINITY, 0.f);
+                    y[k] = in ? *reinterpret_cast<const float4*>(smem_gen + k * SLOTS * kA8StageBytes + (r * kA8OStride + 4 * lane) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    top = fmaxf(top, ml[k].x);
+                }
                 float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-                const float* from = reinterpret_cast<const float*>(smem_gen + k0 * SLOTS * kA8StageBytes) + r * kA8OStride + 4 * lane;
-#pragma unroll 3
-                for (int j = 0; j < k1 - k0; ++j, from += SLOTS * (kA8StageBytes / 4)) {
-                    const float4 y = *reinterpret_cast<const float4*>(from);
-                    const float f = __shfl_sync(0xffffffffu, by, j);
-                    x.x = fmaf(y.x, f, x.x); x.y = fmaf(y.y, f, x.y); x.z = fmaf(y.z, f, x.z); x.w = fmaf(y.w, f, x.w);
+#pragma unroll
+                for (int k = 0; k < KG; ++k) {
+                    const float by = ml[k].x == -INFINITY ? 0.f : ptx::ex2(ml[k].x - top), f = by * s_scale[k];
+                    sum = fmaf(ml[k].y, by, sum);
+                    x.x = fmaf(y[k].x, f, x.x); x.y = fmaf(y[k].y, f, x.y); x.z = fmaf(y[k].z, f, x.z); x.w = fmaf(y[k].w, f, x.w);
                 }
                 if (whole) {
                     const long at = out_row8(a, lens, w, r);
-                    reinterpret_cast<uint2*>(a.out + at * 128)[lane] = make_uint2(ptx::pack_bf16x2(x.x, x.y), ptx::pack_bf16x2(x.z, x.w));
+                    const float by = sum == 0.f ? 0.f : 1.f / sum;
+                    reinterpret_cast<uint2*>(a.out + at * 128)[lane] = make_uint2(ptx::pack_bf16x2(x.x * by, x.y * by), ptx::pack_bf16x2(x.z * by, x.w * by));
                     if (a.lse_out && lane == 0) a.lse_out[at] = (top + log2f(sum)) * kLn2;
                 } else {
                     const long at = (2L * first_run + 1) * ROWS + r;
