@@ -507,7 +507,10 @@ evlnStatus_t evlnGatherKeys(evlnHandle_t h, const evlnGatherParams* p, int num_k
     a.table_first = p->rope_table_first_pos;
     const int vec = 16 / elem_bytes(p->dtype);
     while ((1 << a.vph_shift) < a.D / 2 / vec) ++a.vph_shift;
-    const dim3 grid((unsigned)ceil_div(num_kept, kGatherKeysThreads / (a.D / 2))), block(kGatherKeysThreads);
+    // a slot's angles a thread, more where the blocks would not all be resident (and so could not form theirs while the kernel before them runs)
+    while ((kGatherKeysThreads / (a.D / 2)) >> (a.log_slots + 1)) ++a.log_slots;
+    while ((1 << a.log_slots) < kGatherKeysSlots && (num_kept + (1 << a.log_slots) - 1) >> a.log_slots > h->num_sms * kGatherKeysBlocks) ++a.log_slots;
+    const dim3 grid((unsigned)ceil_div(num_kept, 1 << a.log_slots)), block(kGatherKeysThreads);
     return launched(h, p->dtype == EVLN_BF16 ? launch_pdl(gather_keys_kernel<__nv_bfloat16>, grid, block, 0, (cudaStream_t)stream, a)
                                              : launch_pdl(gather_keys_kernel<float>, grid, block, 0, (cudaStream_t)stream, a));
 }

@@ -4,8 +4,10 @@
 // largest of the weights in the open range, found digit by digit (11, 11 and 10 bits of the float as an ordered integer): each block
 // counts its keys' digits in shared memory, and the blocks read one another's counts over distributed shared memory, first 64 sums of 32 digits, then the
 // 32 digits in question.  Then one ordered pass writes the slots above the threshold, of those equal to it the lowest, and the protected ends,
-// ascending: scans over counts give every slot its place.
-// Bound: latency, and the instructions that a block has to fetch and issue, each a few times only; so loops stay rolled.  (20656 keys: one block per head
+// ascending: every thread counts its run of slots, and scans over the counts give them their places.
+// Most often the keys with the first 22 bits of the threshold are all kept, and the last digit is not looked for.
+// Bound: latency: loads, meetings of the cluster (0.6 us each, one per digit), reads of other
+// blocks' counts (0.3 us each, so never one after the other); loops stay rolled.  (20656 keys of 4 heads: one block per head
 // 15 us, 21 with its keys in registers and everything unrolled; eight blocks that read all 2048 counts of all, 13.)
 // gather_keys_kernel: a block takes a few working slots for all kv heads: their angles once into shared memory, then every
 // head's chosen key (turned as in rope_append.cuh, or copied) and value.
@@ -68,8 +70,7 @@ select_keys_kernel(const SelectArgs a)
 {
     extern __shared__ uint32_t s_key[];                   // [slice] where it fits
     __shared__ __align__(16) int s_bin[3][kSelectBins];
-    __shared__ int s_group[3][kSelectGroups], s_sum[kSelectGroups];
-    __shared__ int s_found[3][2];
+    __shared__ int s_group[3][kSelectGroups], s_sum[kSelectGroups], s_digit[32];
     __shared__ int s_sure[kSelectThreads / 32], s_same[kSelectThreads / 32], s_total[2];
     const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, csize = gridDim.y, rank = blockIdx.y;
     const float* w = a.weights + (long)g * a.stride;
@@ -104,6 +105,7 @@ select_keys_kernel(const SelectArgs a)
     for (int pass = 0; search && pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 1 ? 21 : 10;
         if (pass > 0) {
+#pragma unroll 4
             for (int j = from + tid; j < to; j += kSelectThreads) {
                 const uint32_t k = key(j);
                 if (k >> above == prefix >> above) atomicAdd(&s_bin[pass][(k >> shift) & (pass == 2 ? 1023 : 2047)], 1);
@@ -123,76 +125,84 @@ select_keys_kernel(const SelectArgs a)
             if ((lane & 7) == 0) s_sum[tid >> 3] = sum;
         }
         __syncthreads();
-        if (warp == 0) {
-            // the group in which the count from the largest digit down reaches `left` (lane: two groups), then the digit
-            const int* sums = csize > 1 ? s_sum : s_group[pass];
-            const int g0 = kSelectGroups - 1 - 2 * lane, n0 = sums[g0], n1 = sums[g0 - 1], upto = warp_scan(n0 + n1);
-            const int who = __ffs(__ballot_sync(0xffffffffu, upto >= left)) - 1;
-            int group = g0, before = upto - n0 - n1;
-            if (before + n0 < left) { --group; before += n0; }
-            group = __shfl_sync(0xffffffffu, group, who);
-            before = __shfl_sync(0xffffffffu, before, who);
-            const int digit = 32 * group + 31 - lane;
-            int n = 0;
-            if (csize > 1) {
-#pragma unroll
-                for (int r = 0; r < kSelectCluster; ++r) n += ld_cluster_int(&s_bin[pass][digit], r);
-            } else {
-                n = s_bin[pass][digit];
+        // every warp for itself: the group in which the count from the largest digit down reaches `left` (lane: two groups), then the digit
+        const int* sums = csize > 1 ? s_sum : s_group[pass];
+        const int g0 = kSelectGroups - 1 - 2 * lane, n0 = sums[g0], n1 = sums[g0 - 1], upto = warp_scan(n0 + n1);
+        const int who = __ffs(__ballot_sync(0xffffffffu, upto >= left)) - 1;
+        int group = g0, before = upto - n0 - n1;
+        if (before + n0 < left) { --group; before += n0; }
+        group = __shfl_sync(0xffffffffu, group, who);
+        before = __shfl_sync(0xffffffffu, before, who);
+        int n;
+        if (csize > 1) {                                  // (a lane that reads all eight blocks' counts, one after the other: 2.4 us a pass)
+            if (tid < 32 * kSelectCluster) {
+                int part = ld_cluster_int(&s_bin[pass][32 * group + (tid >> 3)], tid & 7);
+                for (int o = 1; o < 8; o <<= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+                if ((lane & 7) == 0) s_digit[tid >> 3] = part;
             }
-            const int sum = warp_scan(n), at = __ffs(__ballot_sync(0xffffffffu, before + sum >= left)) - 1;
-            if (lane == at) {
-                s_found[pass][0] = digit;
-                s_found[pass][1] = left - before - (sum - n);
-            }
+            __syncthreads();
+            n = s_digit[31 - lane];
+        } else {
+            n = s_bin[pass][32 * group + 31 - lane];
         }
-        __syncthreads();
-        prefix |= (uint32_t)s_found[pass][0] << shift;
-        left = s_found[pass][1];
+        const int sum = warp_scan(n), at = __ffs(__ballot_sync(0xffffffffu, before + sum >= left)) - 1;
+        prefix |= (uint32_t)(32 * group + 31 - at) << shift;
+        left -= before + __shfl_sync(0xffffffffu, sum - n, at);
+        if (__shfl_sync(0xffffffffu, n, at) == left) {    // all with this prefix are kept: what is left of the digits does not matter
+            --prefix;                                     // (no key is below -infinity's, so no prefix is 0)
+            left = 0;
+            break;
+        }
     }
-    // ---- places: every warp a run of neighbouring slots, 32 at a time ----
-    const int per = ((a.slice + kSelectThreads - 1) / kSelectThreads) * 32, j0 = min(last, first + warp * per), j1 = min(last, j0 + per);
-    int sure = 0, same = 0;                               // this warp's slots kept for certain, and equal to the threshold
-    for (int j = j0 + lane; j - lane < j1; j += 32) {
-        const bool open = j >= from && j < to, end = j < j1 && (!open || all);
+    // ---- places: every thread a run of neighbouring slots ----
+    const int per = (a.slice + kSelectThreads - 1) / kSelectThreads, j0 = min(last, first + tid * per), j1 = min(last, j0 + per);
+    auto look = [&](int j, bool& certain, bool& equal) {  // kept for certain, equal to the threshold
+        const bool open = j >= from && j < to;
         const uint32_t k = open && search ? key(j) : 0u;
-        sure += __popc(__ballot_sync(0xffffffffu, end || (search && j < j1 && k > prefix)));
-        same += __popc(__ballot_sync(0xffffffffu, search && open && j < j1 && k == prefix));
+        certain = !open || all || (search && k > prefix);
+        equal = search && open && k == prefix;
+    };
+    int sure = 0, same = 0;
+#pragma unroll 2
+    for (int j = j0; j < j1; ++j) {
+        bool certain, equal;
+        look(j, certain, equal);
+        sure += certain;
+        same += equal;
     }
-    if (lane == 0) {
-        s_sure[warp] = sure;
-        s_same[warp] = same;
+    const int sure_upto = warp_scan(sure), same_upto = warp_scan(same);
+    if (lane == 31) {
+        s_sure[warp] = sure_upto;
+        s_same[warp] = same_upto;
     }
     __syncthreads();
-    sure = warp_scan(lane < kSelectThreads / 32 ? s_sure[lane] : 0);                     // (every warp for itself)
-    same = warp_scan(lane < kSelectThreads / 32 ? s_same[lane] : 0);
+    const int sure_warps = warp_scan(lane < kSelectThreads / 32 ? s_sure[lane] : 0), same_warps = warp_scan(lane < kSelectThreads / 32 ? s_same[lane] : 0);
     if (tid == 31) {
-        s_total[0] = sure;
-        s_total[1] = same;
+        s_total[0] = sure_warps;
+        s_total[1] = same_warps;
     }
-    sure = warp > 0 ? __shfl_sync(0xffffffffu, sure, warp - 1) : 0;                      // kept, and equal, before this warp's slots
-    same = warp > 0 ? __shfl_sync(0xffffffffu, same, warp - 1) : 0;
+    sure = sure_upto - sure;                              // before this thread's slots
+    same = same_upto - same;
+    const int sure_before = __shfl_sync(0xffffffffu, sure_warps, max(warp - 1, 0)), same_before = __shfl_sync(0xffffffffu, same_warps, max(warp - 1, 0));
+    if (warp > 0) {
+        sure += sure_before;
+        same += same_before;
+    }
     if (csize > 1) {
         cluster_meet();
-        int x = lane < rank ? ld_cluster_int(&s_total[0], lane) : 0, y = lane < rank ? ld_cluster_int(&s_total[1], lane) : 0;
-        for (int o = 1; o < 8; o <<= 1) {
-            x += __shfl_xor_sync(0xffffffffu, x, o);
-            y += __shfl_xor_sync(0xffffffffu, y, o);
-        }
+        int x = lane < 2 * kSelectCluster && (lane & 7) < rank ? ld_cluster_int(&s_total[lane >> 3], lane & 7) : 0;      // sure, then same
+        for (int o = 1; o < 8; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
         sure += __shfl_sync(0xffffffffu, x, 0);
-        same += __shfl_sync(0xffffffffu, y, 0);
+        same += __shfl_sync(0xffffffffu, x, 8);
     }
     int* out = a.kept + (long)g * a.num_kept;
-    const unsigned below = (1u << lane) - 1u;
-    for (int j = j0 + lane; j - lane < j1; j += 32) {
-        const bool open = j >= from && j < to, end = j < j1 && (!open || all);
-        const uint32_t k = open && search ? key(j) : 0u;
-        const bool mine = end || (search && j < j1 && k > prefix), equal = search && open && j < j1 && k == prefix;
-        const unsigned s = __ballot_sync(0xffffffffu, mine), e = __ballot_sync(0xffffffffu, equal);
-        const int turn = same + __popc(e & below);
-        if (mine || (equal && turn < left)) out[sure + __popc(s & below) + min(turn, left)] = j;
-        sure += __popc(s);
-        same += __popc(e);
+#pragma unroll 2
+    for (int j = j0; j < j1; ++j) {
+        bool certain, equal;
+        look(j, certain, equal);
+        if (certain || (equal && same < left)) out[sure + min(same, left)] = j;
+        sure += certain;
+        same += equal;
     }
     if (csize > 1) {
         ptx::cluster_arrive_relaxed();                    // nobody leaves while another block may read its counts
@@ -213,65 +223,68 @@ struct GatherKeysArgs {
     const double2* table;    // optional
     int table_first;
     int vph_shift;           // log2 of the 16-byte vectors per half head vector
+    int log_slots;           // log2 of a block's working slots
 };
 
-constexpr int kGatherKeysThreads = 256;
+constexpr int kGatherKeysThreads = 256, kGatherKeysBlocks = 4, kGatherKeysSlots = 16;      // most slots of a block
 template <typename T>
-__global__ void __launch_bounds__(kGatherKeysThreads, 5)
+__global__ void __launch_bounds__(kGatherKeysThreads, kGatherKeysBlocks)
 gather_keys_kernel(const GatherKeysArgs a)
 {
     constexpr int V = VecTraits<T>::kVec;
-    __shared__ __align__(16) typename Rotation<T>::Angle s_angle[8][Rotation<T>::kAngles];
+    __shared__ __align__(16) typename Rotation<T>::Angle s_angle[kGatherKeysSlots][Rotation<T>::kAngles];
     const int D = a.D, half = D / 2, tid = threadIdx.x, vph = a.vph_shift;
-    const int log_slots = D == 128 ? 2 : 3;               // 4 or 8 working slots a block
-    const int p0 = blockIdx.x << log_slots, j = tid & (half - 1), angle_slot = tid >> (D == 128 ? 6 : 5);
-    // theta^(-2 j / D) as a product of at most six powers.  (Without a table a block is bound by arithmetic in double precision: a sine and
-    // cosine, 80 instructions, an exponential 70 more, 4.4 us of 9 for 4096 slots of 4 heads.)
-    double omega = 1.0;
+    const int log_slots = a.log_slots, p0 = blockIdx.x << log_slots, j = tid & (half - 1);
+    const int slots = min(1 << log_slots, a.num_kept - p0), first_slot = tid >> (D == 128 ? 6 : 5), step = kGatherKeysThreads / half;
+    // Without a table the angles hang on launch parameters only and are formed ahead of the wait: a sine and cosine in double precision, 80
+    // instructions, of theta^(-2 j / D) as a product of at most six powers (an exponential, 70 more).
     if (a.rotate && !a.table) {
+        double omega = 1.0;
 #pragma unroll
         for (int b = 0; b < 6; ++b)
             if ((j >> b) & 1) omega *= a.omega[b];
+#pragma unroll 1
+        for (int s = first_slot; s < slots; s += step) Rotation<T>::put(s_angle[s], j, rope_cos_sin_at(p0 + s, omega));
     }
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     // A work item: a pair of 16-byte vectors (channels e V .., + D/2) of a slot's key or value of one head; a key's lanes, then a value's.
     const int items = a.Hkv << (log_slots + vph + 1);
-    long dst = 0;
-    uint4 x0, x1;
-    bool there = false;
-    auto load = [&](int it) {
+    struct Item { uint4 x0, x1; long dst; bool there; };
+    auto load = [&](int it) -> Item {
         const int row = it >> (vph + 1), e = it & ((1 << vph) - 1), p = p0 + (row & ((1 << log_slots) - 1)), g = row >> log_slots;
-        there = it < items && p < a.num_kept;
-        if (!there) return;
+        Item i;
+        i.x0 = i.x1 = make_uint4(0u, 0u, 0u, 0u);
+        i.dst = 0;
+        i.there = it < items && p < a.num_kept;
+        if (!i.there) return i;
         const int from = a.kept[(long)g * a.num_kept + p];
         const bool good = (unsigned)from < (unsigned)a.src_cap, is_v = (it >> vph) & 1;
-        dst = ((long)g * a.dst_cap + p) * D + e * V;
-        x0 = x1 = make_uint4(0u, 0u, 0u, 0u);
+        i.dst = ((long)g * a.dst_cap + p) * D + e * V;
         if (good) {
             const T* src = (const T*)(is_v ? a.v_src : a.k_src) + ((long)g * a.src_cap + from) * D + e * V;
-            x0 = *reinterpret_cast<const uint4*>(src);
-            x1 = *reinterpret_cast<const uint4*>(src + half);
+            i.x0 = *reinterpret_cast<const uint4*>(src);
+            i.x1 = *reinterpret_cast<const uint4*>(src + half);
         }
         if (e == 0 && is_v && a.w_src) a.w_dst[(long)g * a.dst_cap + p] = good ? a.w_src[(long)g * a.src_cap + from] : 0.f;
+        return i;
     };
-    load(tid);                                            // in flight while the angles are formed
+    Item next = load(tid);                                // in flight while the table is read
     if (a.rotate) {
-        const int p = p0 + angle_slot;
-        if (p < a.num_kept) Rotation<T>::put(s_angle[angle_slot], j, a.table ? a.table[(long)(p - a.table_first) * half + j] : rope_cos_sin_at(p, omega));
+        if (a.table)
+            for (int s = first_slot; s < slots; s += step) Rotation<T>::put(s_angle[s], j, a.table[(long)(p0 + s - a.table_first) * half + j]);
         __syncthreads();
     }
-    for (int it = tid; it < items;) {
-        if (there) {
-            const bool is_v = (it >> vph) & 1;
-            uint4 y0 = x0, y1 = x1;
-            if (a.rotate && !is_v) Rotation<T>::turn(s_angle[(it >> (vph + 1)) & ((1 << log_slots) - 1)], it & ((1 << vph) - 1), x0, x1, y0, y1);
-            T* to = (T*)(is_v ? a.v_dst : a.k_dst) + dst;
-            *reinterpret_cast<uint4*>(to) = y0;
-            *reinterpret_cast<uint4*>(to + half) = y1;
-        }
-        it += kGatherKeysThreads;
-        if (it < items) load(it);
+    for (int it = tid; it < items; it += kGatherKeysThreads) {
+        const Item i = next;
+        next = load(it + kGatherKeysThreads);
+        if (!i.there) continue;
+        const bool is_v = (it >> vph) & 1;
+        uint4 y0 = i.x0, y1 = i.x1;
+        if (a.rotate && !is_v) Rotation<T>::turn(s_angle[(it >> (vph + 1)) & ((1 << log_slots) - 1)], it & ((1 << vph) - 1), i.x0, i.x1, y0, y1);
+        T* to = (T*)(is_v ? a.v_dst : a.k_dst) + i.dst;
+        *reinterpret_cast<uint4*>(to) = y0;
+        *reinterpret_cast<uint4*>(to + half) = y1;
     }
 }
 
