@@ -434,7 +434,7 @@ evlnStatus_t evlnKeyWeights(evlnHandle_t h, const evlnStepParams* p, const void*
     a.div_g = make_fast_div((uint32_t)a.G);
     a.div_hkv = make_fast_div((uint32_t)a.Hkv);
     const bool f32 = p->dtype == EVLN_F32;
-    a.chunk_rows = f32 ? kKwF32Rows : a.rows >= 128 ? 128 : (a.rows + 31) / 32 * 32;
+    a.chunk_rows = f32 ? kKwF32Rows : a.rows >= kKwRows ? kKwRows : (a.rows + 31) / 32 * 32;
     a.chunks = ceil_div(a.rows, a.chunk_rows);
     // few tiles: a cluster of CTAs for each, as many as the SMs (fp32: four blocks an SM) and the chunks allow
     int cluster = 1;

@@ -6,11 +6,13 @@
 // key, and its sum is a loop over columns in its own registers: no shuffles and no atomics, and few rows cost few
 // columns instead of a padded 128-row tile.
 //
-// bf16: S^T = K Q^T on tcgen05 (kind::f16, fp32 sums).  Per CTA, 384 threads: warp 0 loads (TMA, a ring of K tiles and one of
-// query chunks), warp 1 issues, warps 4-11 exponentiate: two groups of four (one warp per TMEM lane quarter) that take the
-// chunks in turn, or whole tiles in turn where a tile is one chunk.  Score buffers: 4 x 128 columns.
+// bf16: S^T = K Q^T on tcgen05 (kind::f16, fp32 sums).  Per CTA, 640 threads: warp 0 loads (TMA, a ring of K tiles and one of
+// query chunks), warp 1 issues, warps 2 and 3 fetch the rows' log-sum-exps, warps 4-19 exponentiate: four groups of four (one warp per TMEM lane
+// quarter), two of which share a chunk of 128 rows, or which take whole tiles in turn where a tile is one chunk.  Score buffers: 4 x 128 columns.
 // Bound: many rows, the special-function unit (16 exponentials a cycle and SM; the products take a quarter of that); few
-// rows, reading the keys once.
+// rows, reading the keys once.  (1372 rows of 4 kv heads over 4292 keys: 13.4 us, 5 of them exponentials; over 20196 46.4.  Two groups that fetched their
+// log-sum-exps themselves, and masked every block of a tile that some row does not see, took 15.3 and 58.8: a wait that has to poll costs 0.1 us,
+// a fetch 0.3 us.  Chunks of 64 rows are bound by the issuing warp, 17.9.)
 // Few tiles: the chunks of a tile are dealt to the CTAs of a cluster, whose sums meet in the first one's shared memory, in order.
 // fp32: a thread per key with its row in registers, query rows broadcast from shared memory, float FMAs.
 #pragma once
@@ -37,14 +39,15 @@ struct KeyWeightArgs {
     FastDiv div_g, div_hkv;
 };
 
-constexpr int kKwThreads = 384, kKwStages = 3, kKwBufs = 4, kKwMaxCluster = 8;
+constexpr int kKwGroups = 4, kKwThreads = 128 + 128 * kKwGroups, kKwStages = 3, kKwQStages = 3, kKwBufs = 4, kKwMaxCluster = 8;
+constexpr int kKwRows = 128;                              // most query rows of a chunk (fewer: a multiple of 32)
 template <int D>
 struct KeyWeightPlan {
-    static constexpr int kTile = 128 * D * 2;            // a K tile, a chunk of 128 query rows
-    static constexpr int kQOff = kKwStages * kTile, kBarOff = 2 * kKwStages * kTile;
-    static constexpr int kLseOff = kBarOff + 256;        // float [2 groups][2][128]
-    static constexpr int kPartOff = kLseOff + 2 * 2 * 128 * 4;       // float [2][128]: group 1's sums, tiles in turn
-    static constexpr int kRemoteOff = kPartOff + 2 * 128 * 4;        // float [kKwMaxCluster][128]
+    static constexpr int kTile = 128 * D * 2, kChunk = kKwRows * D * 2;
+    static constexpr int kQOff = kKwStages * kTile, kBarOff = kQOff + kKwQStages * kChunk;
+    static constexpr int kLseOff = kBarOff + 512;        // float [kKwBufs][kKwRows]
+    static constexpr int kPartOff = kLseOff + kKwBufs * kKwRows * 4;             // float [2][kKwGroups - 1][128]: the other groups' sums, tiles in turn
+    static constexpr int kRemoteOff = kPartOff + 2 * (kKwGroups - 1) * 128 * 4;  // float [kKwMaxCluster][128]
     // (never two CTAs on an SM: each takes all of tensor memory, and CTAs of a cluster wait for each other)
     static constexpr int kNeeded = kRemoteOff + kKwMaxCluster * 128 * 4 + 1024, kBytes = kNeeded < 120 * 1024 ? 120 * 1024 : kNeeded;
     static_assert(kBytes <= 227 * 1024, "shared memory of a block");
@@ -66,9 +69,10 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
     const uint32_t bar_k_full = smem_base + Plan::kBarOff, bar_k_empty = bar_k_full + 8 * kKwStages;
-    const uint32_t bar_q_full = bar_k_empty + 8 * kKwStages, bar_q_empty = bar_q_full + 8 * kKwStages;
-    const uint32_t bar_s_full = bar_q_empty + 8 * kKwStages, bar_s_free = bar_s_full + 8 * kKwBufs;
-    const uint32_t tmem_slot = bar_s_free + 8 * kKwBufs;
+    const uint32_t bar_q_full = bar_k_empty + 8 * kKwStages, bar_q_empty = bar_q_full + 8 * kKwQStages;
+    const uint32_t bar_s_full = bar_q_empty + 8 * kKwQStages, bar_s_free = bar_s_full + 8 * kKwBufs;
+    const uint32_t bar_l_full = bar_s_free + 8 * kKwBufs, bar_l_free = bar_l_full + 8 * kKwBufs;
+    const uint32_t tmem_slot = bar_l_free + 8 * kKwBufs;
     volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(smem_gen + (tmem_slot - smem_base));
     volatile int* s_abort = reinterpret_cast<volatile int*>(smem_gen + (tmem_slot - smem_base) + 4);
     float* s_lse = reinterpret_cast<float*>(smem_gen + Plan::kLseOff);
@@ -77,7 +81,7 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // A CTA (cluster size 1) takes tiles blockIdx.x, + gridDim.x, ...; a cluster of several takes one, its chunks dealt out.
-    const int csize = (int)gridDim.y, rank = (int)blockIdx.y, stride = (int)gridDim.x;
+    const int csize = (int)gridDim.y, rank = (int)blockIdx.y, stride = (int)gridDim.x, cshift = __ffs(csize) - 1;
     auto tile_of = [&](int item, int& g) -> int {         // kv heads side by side
         const int t = (int)fast_div((uint32_t)item, a.div_hkv);
         g = item - t * a.Hkv;
@@ -90,12 +94,16 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         for (int i = 0; i < kKwStages; ++i) {
             ptx::mbar_init(bar_k_full + 8 * i, 1);
             ptx::mbar_init(bar_k_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < kKwQStages; ++i) {
             ptx::mbar_init(bar_q_full + 8 * i, 1);
             ptx::mbar_init(bar_q_empty + 8 * i, 1);
         }
         for (int i = 0; i < kKwBufs; ++i) {
             ptx::mbar_init(bar_s_full + 8 * i, 1);
-            ptx::mbar_init(bar_s_free + 8 * i, 4);
+            ptx::mbar_init(bar_s_free + 8 * i, a.chunks == 1 ? 4 : 8);
+            ptx::mbar_init(bar_l_full + 8 * i, 1);
+            ptx::mbar_init(bar_l_free + 8 * i, a.chunks == 1 ? 4 : 8);
         }
         ptx::fence_barrier_init();
         *s_abort = 0;
@@ -129,12 +137,12 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
                         for (int d = 0; d < D; d += 64) ptx::tma_load_3d(smem_base + ks * Plan::kTile + d * 256, &tm_k, bar_k_full + 8 * ks, d, key0, g);
                         fresh = false;
                     }
-                    const int qs = qt % kKwStages;
-                    if (qt >= kKwStages) ok = wait_bounded(bar_q_empty + 8 * qs, ((qt / kKwStages) & 1) ^ 1, kDevTimeoutProducer, a.status, s_abort);
+                    const int qs = qt % kKwQStages;
+                    if (qt >= kKwQStages) ok = wait_bounded(bar_q_empty + 8 * qs, ((qt / kKwQStages) & 1) ^ 1, kDevTimeoutProducer, a.status, s_abort);
                     if (!ok) break;
                     ptx::mbar_expect_tx(bar_q_full + 8 * qs, a.chunk_rows * D * 2);
                     for (int d = 0; d < D; d += 64)
-                        ptx::tma_load_3d(smem_base + Plan::kQOff + qs * Plan::kTile + d * 256, &tm_q, bar_q_full + 8 * qs, d, c * a.chunk_rows, g);
+                        ptx::tma_load_3d(smem_base + Plan::kQOff + qs * Plan::kChunk + d * (kKwRows * 2), &tm_q, bar_q_full + 8 * qs, d, c * a.chunk_rows, g);
                 }
                 if (fresh) --kt;                          // no chunk of this CTA's: the tile was not loaded
             }
@@ -145,113 +153,146 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         }
         __syncwarp();
     } else if (warp == 1) {
-        const uint32_t idesc = make_idesc(false, 128, a.chunk_rows);
-        const uint64_t kd0 = make_sdesc(smem_base, 16, 1024), qd0 = make_sdesc(smem_base + Plan::kQOff, 16, 1024);
-        int kt = 0, qt = 0;
-        for (int item = blockIdx.x; item < a.items && ok; item += stride) {
-            int g;
-            const int key0 = tile_of(item, g), ks = kt % kKwStages, c0 = first_chunk(a, key0) + rank;
-            for (int c = c0; c < a.chunks && ok; c += csize, ++qt) {
-                const int qs = qt % kKwStages, buf = qt % kKwBufs;
-                bool mine = true;
-                if (lane == 0 && c == c0) mine = wait_bounded(bar_k_full + 8 * ks, (kt / kKwStages) & 1, kDevTimeoutMmaKV, a.status, s_abort);
-                if (lane == 1) mine = wait_bounded(bar_q_full + 8 * qs, (qt / kKwStages) & 1, kDevTimeoutMmaQ, a.status, s_abort);
-                if (lane == 2 && qt >= kKwBufs) mine = wait_bounded(bar_s_free + 8 * buf, ((qt / kKwBufs) & 1) ^ 1, kDevTimeoutMmaP, a.status, s_abort);
-                ok = __all_sync(0xffffffffu, mine);
-                if (!ok) break;
-                ptx::fence_after_sync();
-                if (ptx::elect_one()) {
-                    const uint64_t kd = kd0 + (uint64_t)((ks * Plan::kTile) >> 4), qd = qd0 + (uint64_t)((qs * Plan::kTile) >> 4);
+        if (lane == 0) {
+            const uint32_t idesc = make_idesc(false, 128, a.chunk_rows);
+            const uint64_t kd0 = make_sdesc(smem_base, 16, 1024), qd0 = make_sdesc(smem_base + Plan::kQOff, 16, 1024);
+            int kt = 0, qt = 0;
+            for (int item = blockIdx.x; item < a.items && ok; item += stride) {
+                int g;
+                const int key0 = tile_of(item, g), ks = kt % kKwStages, c0 = first_chunk(a, key0) + rank;
+                for (int c = c0; c < a.chunks; c += csize, ++qt) {
+                    const int qs = qt % kKwQStages, buf = qt % kKwBufs;
+                    if (c == c0) ok = wait_bounded(bar_k_full + 8 * ks, (kt / kKwStages) & 1, kDevTimeoutMmaKV, a.status, s_abort);
+                    ok = ok && wait_bounded(bar_q_full + 8 * qs, (qt / kKwQStages) & 1, kDevTimeoutMmaQ, a.status, s_abort);
+                    if (qt >= kKwBufs) ok = ok && wait_bounded(bar_s_free + 8 * buf, ((qt / kKwBufs) & 1) ^ 1, kDevTimeoutMmaP, a.status, s_abort);
+                    if (!ok) break;
+                    ptx::fence_after_sync();
+                    const uint64_t kd = kd0 + (uint64_t)((ks * Plan::kTile) >> 4), qd = qd0 + (uint64_t)((qs * Plan::kChunk) >> 4);
 #pragma unroll
                     for (int s = 0; s < D / 16; ++s) {
-                        const uint64_t off = (uint64_t)(((s >> 2) * 64 * 256 + (s & 3) * 32) >> 4);
-                        ptx::mma_ss(tmem + buf * 128, kd + off, qd + off, idesc, s > 0);
+                        const uint64_t k_off = (uint64_t)(((s >> 2) * 64 * 256 + (s & 3) * 32) >> 4);
+                        const uint64_t q_off = (uint64_t)(((s >> 2) * 64 * (kKwRows * 2) + (s & 3) * 32) >> 4);
+                        ptx::mma_ss(tmem + buf * kKwRows, kd + k_off, qd + q_off, idesc, s > 0);
                     }
                     ptx::mma_commit(bar_s_full + 8 * buf);
                     ptx::mma_commit(bar_q_empty + 8 * qs);
                     if (c + csize >= a.chunks) ptx::mma_commit(bar_k_empty + 8 * ks);
                 }
-                __syncwarp();
+                if (c0 < a.chunks) ++kt;
             }
-            if (c0 < a.chunks) ++kt;
         }
-    } else if (warp >= 4) {
+        __syncwarp();
+    } else if (warp < 4) {
+        // the rows' log-sum-exps, negative and in base 2, of every second chunk: a row behind the last one counts as nothing
+        int qt = 0;
+        for (int item = blockIdx.x; item < a.items && ok; item += stride) {
+            int g;
+            const int key0 = tile_of(item, g);
+            for (int c = first_chunk(a, key0) + rank; c < a.chunks && ok; c += csize, ++qt) {
+                if ((qt & 1) != warp - 2) continue;
+                const int buf = qt % kKwBufs, row0 = c * a.chunk_rows;
+                float mine[kKwRows / 32];
+#pragma unroll
+                for (int i = 0; i < kKwRows / 32; ++i) {
+                    const int r = row0 + 32 * i + lane, tok = (int)fast_div((uint32_t)r, a.div_g);
+                    mine[i] = 32 * i < a.chunk_rows && r < a.rows ? a.lse[(long)tok * (a.Hkv * a.G) + g * a.G + (r - tok * a.G)] : INFINITY;
+                }
+                if (qt >= kKwBufs) ok = warp_wait(bar_l_free + 8 * buf, ((qt / kKwBufs) & 1) ^ 1, kDevTimeoutProducer, a.status, s_abort, lane);
+                if (!ok) break;
+#pragma unroll
+                for (int i = 0; i < kKwRows / 32; ++i) s_lse[buf * kKwRows + 32 * i + lane] = mine[i] * -1.4426950408889634f;
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(bar_l_full + 8 * buf);
+            }
+        }
+    } else {
         const int quarter = warp & 3, grp = (warp - 4) >> 2;
         const int key_lane = (quarter << 5) + lane;       // = TMEM lane = the thread's key within a tile
         const uint32_t t_lane = tmem + ((uint32_t)(quarter << 5) << 16);
-        float* my_lse = s_lse + grp * 256;
-        const bool turns = a.chunks == 1;                 // whole tiles in turn
+        // one chunk a tile: the groups take the tiles in turn; else two take every second chunk, half of it each
+        const bool turns = a.chunks == 1;
+        const int col0 = turns ? 0 : (grp & 1) * (kKwRows / 2), col1 = turns ? a.chunk_rows : col0 + kKwRows / 2;
         const uint64_t scale2 = ptx::pack2(a.scale_log2, a.scale_log2);
-        int qt = 0, kt = 0, used = 0;                     // chunks, tiles; chunks of this group
-        auto meet = [&](int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); };
+        int qt = 0, kt = 0;                               // chunks, tiles
         for (int item = blockIdx.x; item < a.items; item += stride) {
             int g;
             const int key0 = tile_of(item, g), key = key0 + key_lane, c0 = first_chunk(a, key0) + rank;
-            const bool writes = key < a.L + a.n && rank == 0 && (turns ? (kt & 1) == grp : grp == 0);
-            const float had = writes && key < a.L ? a.in[(long)g * a.cap + key] * a.decay : 0.f;
+            const bool writes = key < a.L + a.n && rank == 0 && grp == (turns ? kt % kKwGroups : 0);
+            const float had = writes && key < a.L ? a.in[(long)g * a.cap + key] : 0.f;
             const int from = key > a.L ? (key - a.L) * a.G : 0;           // the first row that sees the key
             const bool edge = key0 + kTileN - 1 > a.L;                    // (uniform) some key of the tile is not seen by all
             uint64_t sum0 = 0, sum1 = 0;                                  // two floats each
-            for (int c = c0; c < a.chunks; c += csize, ++qt) {
-                if ((turns ? (kt & 1) : (qt & 1)) != grp) continue;
-                const int buf = qt % kKwBufs, row0 = c * a.chunk_rows, valid = min(a.chunk_rows, a.rows - row0);
-                float* lse = my_lse + (used & 1) * 128;
-                ++used;
-                float mine = INFINITY;                    // a row behind the last one counts as nothing
-                if (key_lane < valid) {
-                    const int r = row0 + key_lane, i = (int)fast_div((uint32_t)r, a.div_g);
-                    mine = a.lse[(long)i * (a.Hkv * a.G) + g * a.G + (r - i * a.G)] * 1.4426950408889634f;
+            const int count = c0 < a.chunks ? (a.chunks - c0 + csize - 1) >> cshift : 0;
+            const int first = turns ? (kt % kKwGroups == grp ? 0 : count) : ((grp >> 1) ^ qt) & 1;
+            for (int i = first; i < count; i += 2) {
+                const int at = qt + i, buf = at % kKwBufs, row0 = (c0 + i * csize) * a.chunk_rows, valid = min(a.chunk_rows, a.rows - row0);
+                const uint32_t parity = (at / kKwBufs) & 1;
+                const float* lse = s_lse + buf * kKwRows;
+                const uint32_t have = ptx::mbar_try_wait(bar_l_full + 8 * buf, parity) & ptx::mbar_try_wait(bar_s_full + 8 * buf, parity);
+                if (!__all_sync(0xffffffffu, have)) {                     // (seldom: and 0.2 us more)
+                    ok = ok && warp_wait(bar_l_full + 8 * buf, parity, kDevTimeoutSoftmaxS, a.status, s_abort, lane);
+                    ok = ok && warp_wait(bar_s_full + 8 * buf, parity, kDevTimeoutSoftmaxS, a.status, s_abort, lane);
+                    __syncwarp();
                 }
-                lse[key_lane] = -mine;
-                meet(1 + grp, 128);                       // (the other buffer's readers are done: they met here since)
-                ok = ok && warp_wait(bar_s_full + 8 * buf, (qt / kKwBufs) & 1, kDevTimeoutSoftmaxS, a.status, s_abort, lane);
-                if (ok) {
-                    ptx::fence_after_sync();
-                    const bool plain = !edge && valid == a.chunk_rows;
-                    for (int col = 0; col < a.chunk_rows; col += 32) {
-                        uint32_t s[32];
-                        ptx::tmem_ld32(t_lane + buf * 128 + col, s);
-                        ptx::tmem_ld_wait();
-                        if (col + 32 >= a.chunk_rows) {
-                            ptx::fence_before_sync();
-                            if (ptx::elect_one()) ptx::mbar_arrive(bar_s_free + 8 * buf);
+                if (!ok) break;
+                ptx::fence_after_sync();
+                const bool plain = !edge && valid == a.chunk_rows;
+#pragma unroll 1
+                for (int col = col0; col < col1; col += 32) {
+                    uint32_t s[32];
+                    ptx::tmem_ld32(t_lane + buf * kKwRows + col, s);
+                    ptx::tmem_ld_wait();
+                    if (col + 32 >= col1) {
+                        ptx::fence_before_sync();
+                        if (ptx::elect_one()) ptx::mbar_arrive(bar_s_free + 8 * buf);
+                    }
+                    const float4* l4 = reinterpret_cast<const float4*>(lse + col);
+                    const int lo = from - row0 - col, hi = valid - col;   // columns lo .. hi-1 count
+                    if (plain || __all_sync(0xffffffffu, lo <= 0 && hi >= 32)) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) {
+                            const float4 m = l4[e >> 2];
+                            float x0, x1, x2, x3;
+                            ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), scale2, ptx::pack2(m.x, m.y)), x0, x1);
+                            ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), scale2, ptx::pack2(m.z, m.w)), x2, x3);
+                            sum0 = ptx::add2(sum0, ptx::pack2(ptx::ex2(x0), ptx::ex2(x1)));
+                            sum1 = ptx::add2(sum1, ptx::pack2(ptx::ex2(x2), ptx::ex2(x3)));
                         }
-                        const float4* l4 = reinterpret_cast<const float4*>(lse + col);
-                        if (plain) {
+                    } else if (__any_sync(0xffffffffu, lo < 32 && hi > 0)) {
+                        const uint32_t count_in = (hi >= 32 ? ~0u : hi <= 0 ? 0u : (1u << hi) - 1u) & (lo <= 0 ? ~0u : lo >= 32 ? 0u : ~0u << lo);
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4) {
-                                const float4 m = l4[e >> 2];
-                                float x0, x1, x2, x3;
-                                ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), scale2, ptx::pack2(m.x, m.y)), x0, x1);
-                                ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), scale2, ptx::pack2(m.z, m.w)), x2, x3);
-                                sum0 = ptx::add2(sum0, ptx::pack2(ptx::ex2(x0), ptx::ex2(x1)));
-                                sum1 = ptx::add2(sum1, ptx::pack2(ptx::ex2(x2), ptx::ex2(x3)));
-                            }
-                        } else {
-                            const int lo = from - row0 - col, hi = valid - col;       // columns lo .. hi-1 count
-                            float add = 0.f;
+                        for (int e = 0; e < 32; e += 4) {
+                            const float4 m = l4[e >> 2];
+                            const float in[4] = {m.x, m.y, m.z, m.w};
+                            float x[4];
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) {
-                                const float p = ptx::ex2(fmaf(__uint_as_float(s[e]), a.scale_log2, lse[col + e]));
-                                add += e >= lo && e < hi ? p : 0.f;
+                            for (int o = 0; o < 4; ++o) {
+                                const float x_all = ptx::ex2(fmaf(__uint_as_float(s[e + o]), a.scale_log2, in[o]));
+                                x[o] = count_in & (1u << (e + o)) ? x_all : 0.f;
                             }
-                            sum0 = ptx::add2(sum0, ptx::pack2(add, 0.f));
+                            sum0 = ptx::add2(sum0, ptx::pack2(x[0], x[1]));
+                            sum1 = ptx::add2(sum1, ptx::pack2(x[2], x[3]));
                         }
                     }
                 }
+                __syncwarp();
+                if (ptx::elect_one()) ptx::mbar_arrive(bar_l_free + 8 * buf);
             }
+            qt += count;
             float u0, u1, u2, u3;
             ptx::unpack2(sum0, u0, u1);
             ptx::unpack2(sum1, u2, u3);
             float sum = (u0 + u1) + (u2 + u3);
             if (!turns) {
-                float* part = s_part + (kt & 1) * 128;
-                if (grp == 1) part[key_lane] = sum;
-                meet(3, 256);
-                if (grp == 0) sum += part[key_lane];
+                float* part = s_part + (kt & 1) * ((kKwGroups - 1) * 128) + key_lane;
+                if (grp > 0) part[(grp - 1) * 128] = sum;
+                asm volatile("bar.sync 1, %0;" :: "n"(128 * kKwGroups) : "memory");
+                if (grp == 0)
+#pragma unroll
+                    for (int o = 0; o < kKwGroups - 1; ++o) sum += part[o * 128];
             }
             if (csize > 1) own_sum = sum;
-            else if (writes && ok) a.out[(long)g * a.cap + key] = had + sum;
+            else if (writes && ok) a.out[(long)g * a.cap + key] = fmaf(had, a.decay, sum);
             ++kt;
         }
     }
