@@ -116,7 +116,7 @@ def physical_gpu_index(local_index: int) -> int:
 # ------------------------------------------------------------------------------------------------
 
 MIN_REPLAYS = 200           # every timed graph is replayed at least this often, whatever --steps says
-K2_SOURCES = ("attn_pair.cuh", "ptx_sm100.cuh", "common.cuh")
+K2_SOURCES = ("attn_pair.cuh", "tc_common.cuh", "ptx_sm100.cuh", "common.cuh")
 K2_TRAFFIC_FILE = os.path.join(ROOT, "profiles", "attn_pair_kernel_step_7b_L4096.traffic.txt")
 
 

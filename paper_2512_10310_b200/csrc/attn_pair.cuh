@@ -417,7 +417,7 @@ __device__ __forceinline__ void write_rows(const TcAttnArgs& a, const LensT& len
 // that cache (every row sees all of them) and bring their own n_b new tokens in a separate buffer
 // (tm_qt / tm_kt / tm_vt, packed over the batch; causal among themselves), each after its own prefix of
 // the visual tokens, none visible to another.
-template <bool PAGED, bool TAIL, bool PERSIST, typename LensT, int CTAS, typename TableT>
+template <bool PAGED, bool TAIL, bool PERSIST, typename LensT, int CTAS, typename TableT, bool POLY = !(PAGED && PERSIST)>
 __device__ __forceinline__ void attn_tc_body(const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                                              const CUtensorMap* tm_qt, const CUtensorMap* tm_kt, const CUtensorMap* tm_vt,
                                              const TcAttnArgs& a, const LensT& lens, const TcOutArgs& d, const TableT& table)
@@ -1078,7 +1078,7 @@ __device__ __forceinline__ void attn_tc_body(const CUtensorMap& tm_q, const CUte
             uint64_t sum2a = ptx::pack2(0.f, 0.f), sum2b = sum2a;
             {
                 uint32_t pk[16];
-                exp32<!(PAGED && PERSIST)>(&s[0], pk, scale2, negm2, sum2a, sum2b);
+                exp32<POLY>(&s[0], pk, scale2, negm2, sum2a, sum2b);
                 while (ok && gj >= 2) {
                     const int r = wait_or_request(bar_pv_done + 8 * ((gj - 2) & 3), ((gj - 2) >> 2) & 1, kDevTimeoutSoftmaxO);
                     if (r == 0) break;
@@ -1111,7 +1111,7 @@ __device__ __forceinline__ void attn_tc_body(const CUtensorMap& tm_q, const CUte
                 const float neg_m2 = (m_ref == -INFINITY) ? 0.f : -m_ref;
                 const uint64_t negm2b = ptx::pack2(neg_m2, neg_m2);
                 uint32_t pk[16];
-                exp32<!(PAGED && PERSIST)>(&s[32], pk, scale2, negm2b, sum2a, sum2b);
+                exp32<POLY>(&s[32], pk, scale2, negm2b, sum2a, sum2b);
                 ptx::tmem_st16(t_p + 16, pk);
             }
             {
@@ -1192,12 +1192,15 @@ attn_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 // A CTA pair per work item of a batch of paged episodes that has no more of them than pairs.
 // (The persistent kernel below takes about 1 us longer for its only item: it decodes a list of them first and has
 // the shallower V ring: 28/4 heads, 196 tokens over 9000 keys 33.5 us against 32.0, 20 tokens 16.3 and 15.2.)
+// POLY false: over the copy of a cache in 8 bits, where log-sum-exps of a few keys are to be good to 2^-20 as they are from the codes
+// (the cubic's 2^-13 leaves 5e-6 of them; with copy and all, 16 tokens of 28/4 heads over 4096 keys 18.1 us, 17.7 with the cubic, 196 26.1 and 26.0).
+template <bool POLY>
 __global__ void __launch_bounds__(kTcThreads, 1)
 attn_paged_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                        const __grid_constant__ CUtensorMap tm_v, const TcAttnArgs a, const __grid_constant__ PagedLens lens,
                        const __grid_constant__ TcOutArgs d)
 {
-    attn_tc_body<true, false, false, PagedLens, 2, NoTable>(tm_q, tm_k, tm_v, nullptr, nullptr, nullptr, a, lens, d, NoTable{});
+    attn_tc_body<true, false, false, PagedLens, 2, NoTable, POLY>(tm_q, tm_k, tm_v, nullptr, nullptr, nullptr, a, lens, d, NoTable{});
 }
 
 // At most one CTA pair per two SMs, each going through several work items: more items than pairs, on a

@@ -99,8 +99,9 @@ cudaError_t prepare_few()
 // Shared-memory limits of the kernels that take more than the default, on the current device.
 cudaError_t prepare_kernels()
 {
-    const std::pair<const void*, int> tc[6] = {{(const void*)attn_pair_kernel, kTcSmemBytes},
-                                               {(const void*)attn_paged_pair_kernel, kTcSmemBytes},
+    const std::pair<const void*, int> tc[7] = {{(const void*)attn_pair_kernel, kTcSmemBytes},
+                                               {(const void*)attn_paged_pair_kernel<true>, kTcSmemBytes},
+                                               {(const void*)attn_paged_pair_kernel<false>, kTcSmemBytes},
                                                {(const void*)attn_persistent_kernel<false, NoLens>, kPersistSmemBytes},
                                                {(const void*)attn_persistent_kernel<true, PagedLens>, kPersistSmemBytes},
                                                {(const void*)attn_solo_kernel, kSoloSmemBytes},
@@ -130,7 +131,7 @@ cudaError_t prepare_kernels()
 bool attention_register_pool_ok()
 {
     cudaFuncAttributes fa;
-    const void* kernels[6] = {(const void*)attn_pair_kernel, (const void*)attn_paged_pair_kernel, (const void*)attn_persistent_kernel<false, NoLens>, (const void*)attn_persistent_kernel<true, PagedLens>,
+    const void* kernels[7] = {(const void*)attn_pair_kernel, (const void*)attn_paged_pair_kernel<true>, (const void*)attn_paged_pair_kernel<false>, (const void*)attn_persistent_kernel<false, NoLens>, (const void*)attn_persistent_kernel<true, PagedLens>,
                               (const void*)attn_solo_kernel, (const void*)attn_packed_kernel};
     for (const void* k : kernels) {
         if (cudaFuncGetAttributes(&fa, k) != cudaSuccess) return false;
@@ -1587,7 +1588,9 @@ static evlnStatus_t paged_attention(evlnHandle_t h, const evlnPagedParams* p, co
         d.lse_out = out ? lse_out : a.lse_part;
     }
     if (items <= persistent_pairs(h, items)) {
-        const cudaError_t e = launch_pair_pdl(attn_paged_pair_kernel, dim3(2 * (unsigned)items), kTcSmemBytes, (cudaStream_t)stream, tm_q, tm_k, tm_v, a, bl, d);
+        const dim3 grid(2 * (unsigned)items);
+        const cudaError_t e = out ? launch_pair_pdl(attn_paged_pair_kernel<false>, grid, kTcSmemBytes, (cudaStream_t)stream, tm_q, tm_k, tm_v, a, bl, d)
+                                  : launch_pair_pdl(attn_paged_pair_kernel<true>, grid, kTcSmemBytes, (cudaStream_t)stream, tm_q, tm_k, tm_v, a, bl, d);
         return e == cudaSuccess ? EVLN_OK : cuda_fail(h, e);
     }
     ItemTable table;
