@@ -459,7 +459,8 @@ evlnStatus_t evlnPagedNormRopeAppend(evlnHandle_t handle, const evlnPagedParams*
  * the largest code, NaN as NaN, and neither counts for the scale.  Value slots behind the episode's last token are
  * cleared up to the end of its page; key slots there, and pages that no new token goes to, are left as they were.
  *
- * evlnPaged8StepAttention: causal attention of the rotated queries over such a cache, out and lse_out (may be NULL) as
+ * evlnPaged8StepAttention: causal attention of the rotated queries over such a cache (the scales of its pages are powers
+ * of two, as evlnPaged8RopeAppend leaves them; other scales give undefined numbers), out and lse_out (may be NULL) as
  * from evlnPagedStepAttention + evlnPagedStepCombine.  Up to 64 query rows per kv head are read from the codes
  * themselves, more are served from a bf16 copy of the batch's pages in the workspace (exact: code * scale is a bf16
  * number), so that evlnPaged8WorkspaceSize is larger for those.                                            */

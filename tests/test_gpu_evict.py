@@ -48,6 +48,11 @@ def _weights_case(dtype, hq, hkv, D, L, n, cap, seed, scale):
     ("bf16", 2, 1, 64, 0, 300, 1.0, 0.3),           # an empty cache: every key has its own rows
     ("bf16", 6, 2, 64, 127, 129, 1.0, 0.0),
     ("bf16", 5, 5, 128, 128, 128, 0.7, 0.05),
+    ("bf16", 28, 4, 128, 100, 196, 1.0, 0.0),       # most tiles have keys that only some rows see
+    ("bf16", 16, 2, 128, 30000, 17, 1.0, 0.0),      # three chunks of a tile, the last one short
+    ("bf16", 16, 1, 64, 20000, 9, 0.5, 0.0),        # two chunks, several tiles a CTA
+    ("bf16", 4, 4, 64, 9000, 127, 1.0, 0.0),        # one chunk of 127 rows
+    ("bf16", 4, 4, 128, 9000, 128, 1.0, 0.0),       # one whole chunk, tiles in turn
     ("f32", 2, 1, 64, 256, 64, 0.9, 0.0),
     ("f32", 28, 4, 128, 300, 7, 1.0, 0.0),
     ("f32", 3, 3, 128, 0, 1, 1.0, 0.0),
