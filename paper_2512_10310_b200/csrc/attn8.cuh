@@ -113,6 +113,15 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
     return r;
 }
 
+// warp_wait for a barrier that has most often completed: every lane looks once, which takes 0.1 us less than one lane's polling and sharing.
+__device__ __forceinline__ bool warp_wait_ready(uint32_t bar, uint32_t parity, int code, int* status, volatile int* s_abort, int lane)
+{
+    if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity))) return true;
+    const bool ok = warp_wait(bar, parity, code, status, s_abort, lane);
+    __syncwarp();
+    return ok;
+}
+
 // Where query row rl of a unit goes: row of [tokens, Hq].
 __device__ __forceinline__ long out_row8(const Attn8Args& a, const BatchLens& lens, const Unit8& u, int rl)
 {
@@ -270,7 +279,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             const uint32_t kbase = (ring + slot * kA8StageBytes + lane * 128) ^ ((lane & 7) << 4), vbase = kbase + kA8StageBytes / 2;
             const float ks = __shfl_sync(0xffffffffu, now.ks, i & 31), vs = __shfl_sync(0xffffffffu, now.vs, i & 31);
             const int key0 = (r0 + i - u.first) * kA8Keys;
-            ok = ok && warp_wait(bar_full + 8 * slot, parity, kDevTimeoutMmaKV, a.status, s_abort, lane);
+            ok = ok && warp_wait_ready(bar_full + 8 * slot, parity, kDevTimeoutMmaKV, a.status, s_abort, lane);
             if (ok) {
                 // ---- scores: 16 rows (8 of them used, NQ = 1) x 32 keys ----
                 float sc[4][4];
@@ -372,7 +381,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             if (rg == 0 && i + SLOTS < mine) {
                 const int ahead = i + SLOTS;
                 const int row = __shfl_sync(0xffffffffu, (ahead >> 5) == (i >> 5) ? now.row : next.row, ahead & 31);
-                if (RG > 1) ok = ok && warp_wait(bar_empty + 8 * slot, parity, kDevTimeoutProducer, a.status, s_abort, lane);
+                if (RG > 1) ok = ok && warp_wait_ready(bar_empty + 8 * slot, parity, kDevTimeoutProducer, a.status, s_abort, lane);
                 if (ok && lane == 0) load(slot, row);
             }
             if (++slot == SLOTS) {

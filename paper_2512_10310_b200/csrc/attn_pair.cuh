@@ -1193,7 +1193,7 @@ attn_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 // (The persistent kernel below takes about 1 us longer for its only item: it decodes a list of them first and has
 // the shallower V ring: 28/4 heads, 196 tokens over 9000 keys 33.5 us against 32.0, 20 tokens 16.3 and 15.2.)
 // POLY false: over the copy of a cache in 8 bits, where log-sum-exps of a few keys are to be good to 2^-20 as they are from the codes
-// (the cubic's 2^-13 leaves 5e-6 of them; with copy and all, 16 tokens of 28/4 heads over 4096 keys 18.1 us, 17.7 with the cubic, 196 26.1 and 26.0).
+// (the cubic's 2^-13 leaves 5e-6 of them; 16 tokens of 28/4 heads over 4096 keys take 0.4 us longer than with the cubic, 196 0.1).
 template <bool POLY>
 __global__ void __launch_bounds__(kTcThreads, 1)
 attn_paged_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,

@@ -142,9 +142,9 @@ void batch_lens(BatchLens* bl, const evlnPagedParams* p, const int* lens, const 
 
 // ---- attention over the cache in 8 bits ----------------------------------------------------------
 
-// Most query rows of an episode (per kv head) that the kernel on the codes serves: a tile's.  More go through a bf16 copy, which takes the same time for
-// 65 rows as for 250, less than the codes twice.  (us, 64, 128 and 256 rows on the codes, then through the copy: one episode of 4096 keys 17.1, 16.9 and
-// 21.7, 15.6 to 17.3; of 20656 28.2, 36.8, 59.2, 31.2 to 34.7; 16 of 8000 95.8, 175, 327, 139 to 140.)
+// Most query rows of an episode (per kv head) that the kernel on the codes serves: a block's.  More go through a bf16 copy, which takes the same time for
+// 70 rows as for 250, less than the codes twice.  (us, 63 rows on the codes, 70 and 252 through the copy: one episode of 4096 keys 13.3, 14.4 and
+// 16.6; of 20656 21.9, 27.4, 30.8; 16 of 8000 96, 121, 122.)
 constexpr int kA8MostRows = 64;
 
 struct Plan8 {
