@@ -11,7 +11,7 @@
 // norm, rotation and the block's maximum to the codes: one pass.  Codes of earlier tokens are loaded instead of new ones and stored again only
 // if the scale grew.
 // Bound: latency for a token an episode (a chain of loads, the block's maximum, stores: 16 episodes 2.4 us), else the queries' traffic (16 frames of
-// 196 tokens with norms, 56 MB, 18.1 us).  (One token a lane, blocks of 512 threads: 2.7 and 21.4 us.)
+// 196 tokens with norms, 56 MB, 16.9 us).  (One token a lane, blocks of 512 threads: 2.7 and 21.4 us.)
 #pragma once
 
 #include <cuda_fp16.h>
@@ -100,13 +100,13 @@ append8_kernel(const Append8Args p, const __grid_constant__ BatchLens lens)
         ptx::grid_launch_dependents();
         if (tok >= a.num_new) return;
         const int items = a.Hq * kVectors;
-        token_heads<T, NORM>(a, p.norm, s_angles.of_token[wid], tok, 32 * (w - tok * p.q_warps) + (threadIdx.x & 31), 32 * p.q_warps, items, items, items, 0, [&]() -> long {
+        token_heads<T, NORM>(a, p.norm, &s_angles.of_token[wid], tok, 32 * (w - tok * p.q_warps) + (threadIdx.x & 31), 32 * p.q_warps, items, items, items, 0, [&]() -> long {
             int b = 0, hi = a.batch;                          // largest b with new_off[b] <= tok
             while (hi - b > 1) {
                 const int mid = (b + hi) >> 1;
                 if (lens.new_off[mid] <= tok) b = mid; else hi = mid;
             }
-            fill_angles<TABLE>(s_angles.of_token[wid], a, lens.cache_len[b] + tok - lens.new_off[b], omega);
+            fill_angles<T, NORM, TABLE>(&s_angles.of_token[wid], a, p.norm, lens.cache_len[b] + tok - lens.new_off[b], omega, true, false);
             return 0;
         });
         return;
@@ -148,12 +148,10 @@ append8_kernel(const Append8Args p, const __grid_constant__ BatchLens lens)
     }
     const float old_scale = held ? *scale_at : 0.f;
     uint64_t x[2][2][4];                                  // the numbers to store, in pairs
-    uint4 w0 = make_uint4(0u, 0u, 0u, 0u), w1 = w0;
-    const bool weighted = NORM && !is_v && p.norm.k_weight;
-    if (weighted) {
-        w0 = *reinterpret_cast<const uint4*>((const T*)p.norm.k_weight + c0);
-        w1 = *reinterpret_cast<const uint4*>((const T*)p.norm.k_weight + c0 + half);
-    }
+    float w[2][2] = {{1.f, 1.f}, {1.f, 1.f}};             // keys: the weights of channels lane, lane + 64, then lane + 32, lane + 96
+    if (NORM && !is_v)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i & 1][i >> 1] = weight_of<T>(p.norm.k_weight, lane + 32 * i);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         if (is_v) {
@@ -170,12 +168,13 @@ append8_kernel(const Append8Args p, const __grid_constant__ BatchLens lens)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int j = (lane + 32 * i) & (half - 1), pos = first + i / 2;
-            if (pos >= L && pos < L + n) s_angles.of_slots[wid][i / 2].put(j, TABLE ? a.table[(long)(pos - a.table_first) * half + j] : rope_cos_sin(pos, j, D, a.log2_theta));
+            if (pos >= L && pos < L + n)
+                s_angles.of_slots[wid][i / 2].put(j, TABLE ? a.table[(long)(pos - a.table_first) * half + j] : rope_cos_sin(pos, j, D, a.log2_theta), w[i & 1][0], w[i & 1][1]);
         }
         __syncwarp();
         const float inv = NORM ? norm_factor<T>(r0[u], r1[u], 3, D, p.norm.eps) : 1.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) norm_turn_pair<T>(s_angles.of_slots[wid][slot0 & 3], k, i, inv, weighted, w0, w1, r0[u], r1[u], x[u][0][i], x[u][1][i]);
+        for (int i = 0; i < 4; ++i) norm_turn_pair<T>(s_angles.of_slots[wid][slot0 & 3], k, i, inv, r0[u], r1[u], x[u][0][i], x[u][1][i]);
     }
     // the page's maximum; infinities and NaN do not count (an infinity becomes the largest code, NaN a NaN code)
     float most = 0.f;

@@ -6,11 +6,12 @@
 // one warp, a pair of 16-byte vectors (channels j.. and j + D/2..) each: the sum of squares is V packed FMAs and s
 // shuffles, and the pair is what the rotation wants.  Everything after the load is in floats (two channels an instruction) and rounded once,
 // to the storage type: there is no rounding between norm and rotation, as there is where they are two passes.
-// A warp serves one token: it fills the token's angles into its own corner of shared memory, then takes 32 work items after the other, so that no
-// warp waits for another one and the angles' cost is shared.  As many warps per token as are resident together: a second wave costs more than a
-// longer loop (392 tokens of 28 + 8 heads: 9 warps each 4.1 us, 10 warps and two waves 6.2).
-// Bound: for few tokens latency (1.5 us for one), for many HBM: 3136 tokens, 58 MB, 15.2 us = 3.8 TB/s, where the same bytes take 10.4 us in an
-// elementwise pass.  (A block per token with a thread per item issued 2.5 times the instructions and took 19.8 us, blocks of two tokens 17.5.)
+// A warp serves one token: it fills the token's angles, the weights multiplied into them, into its own corner of shared memory, then takes 32 work items
+// after the other, so that no warp waits for another one and the angles' cost is shared.  As many warps per token as are resident together: a second
+// wave costs more than a longer loop (392 tokens of 28 + 8 heads: 9 warps each 4.1 us, 10 warps and two waves 6.2).
+// Bound: for few tokens latency (1.7 us for one), for many HBM: 3136 tokens, 58 MB, 13.9 us = 4.2 TB/s, where the same bytes take 10.4 us in an
+// elementwise pass.  (A block per token with a thread per item issued 2.5 times the instructions and took 19.8 us, blocks of two tokens 17.5; weights
+// multiplied to the numbers instead of to the angles 15.2, and 1.5 for a token.)
 #pragma once
 
 #include "common.cuh"
@@ -19,9 +20,9 @@
 
 namespace evln {
 
-// A block: four warps (of eight, the first of few tokens started later: 1.9 us for a token, 1.5).  The loop keeps 80 registers; with fewer, and so more
-// warps resident, the compiler puts some of it aside (3136 tokens: 15.0 us with 24 warps an SM, 16.4 with 28, 19.0 with 32).
-constexpr int kNormWarps = 4, kNormBlocks = 6;
+// A block: four warps (of eight, the first of few tokens started later: 1.9 us for a token, 1.5).  Seven blocks an SM leave a thread 72 registers, which the
+// loop fits (392 tokens 4.2 us, 4.3 with six blocks, 3136 13.9 with both; eight blocks and 64 registers 15.8: the compiler puts some of it aside).
+constexpr int kNormWarps = 4, kNormBlocks = 7;
 
 struct NormArgs {
     const void* q_weight;    // [D] of the tokens' type, or null: ones
@@ -70,47 +71,51 @@ __device__ __forceinline__ float norm_factor(const uint4& lo, const uint4& hi, i
     return rsqrtf(fmaf(ss, 1.f / (float)D, eps));
 }
 
-// (cos, sin) of a token's D/2 angles in shared memory.  NORM: as floats, (cos, cos, sin, sin) of two channels, the four of eight channels to
-// 80 bytes, so that the lanes of a head start in different banks; else as the rotation of a stored number wants them.
+// A token's D/2 angles in shared memory.  NORM: with the weights w of a head's channels j and j + D/2 in them, for two channels (c w_j, -s w_j'; c w_j',
+// s w_j), the eight vectors of eight channels to 144 bytes, so that the lanes of a head start in different banks; else as the rotation of
+// a stored number wants them.
 template <typename T, bool NORM> struct TokenAngles;
 template <typename T> struct TokenAngles<T, true> {
-    float4 at[40];
-    static __device__ __forceinline__ int place(int pair) { return pair + (pair >> 2); }
-    __device__ __forceinline__ void put(int j, const double2& cs)
+    float4 at[72];
+    static __device__ __forceinline__ int place(int pair) { return 9 * (pair >> 2) + 2 * (pair & 3); }
+    __device__ __forceinline__ void put(int j, const double2& cs, float lo, float hi)
     {
         float* to = reinterpret_cast<float*>(at + place(j >> 1)) + (j & 1);
-        to[0] = (float)cs.x;
-        to[2] = (float)cs.y;
+        const float c = (float)cs.x, s = (float)cs.y;
+        to[0] = c * lo;
+        to[2] = -(s * hi);
+        to[4] = c * hi;
+        to[6] = s * lo;
     }
 };
 template <typename T> struct TokenAngles<T, false> {
     typename Rotation<T>::Angle at[Rotation<T>::kAngles];
     __device__ __forceinline__ void put(int j, const double2& cs) { Rotation<T>::put(at, j, cs); }
 };
-
-// Channels 2 i, 2 i + 1 of a head's vectors lo, hi (vector k of the half), times inv and the weights (if any: w0, w1), turned.
 template <typename T>
-__device__ __forceinline__ void norm_turn_pair(const TokenAngles<T, true>& angles, int k, int i, float inv, bool weighted, const uint4& w0, const uint4& w1,
-                                               const uint4& lo, const uint4& hi, uint64_t& out_lo, uint64_t& out_hi)
+__device__ __forceinline__ float weight_of(const void* weight, int channel)
 {
-    const uint64_t inv2 = ptx::pack2(inv, inv);
-    uint64_t x = ptx::mul2(pair_of<T>(lo, i), inv2), y = ptx::mul2(pair_of<T>(hi, i), inv2);
-    if (weighted) {
-        x = ptx::mul2(x, pair_of<T>(w0, i));
-        y = ptx::mul2(y, pair_of<T>(w1, i));
-    }
-    const float4 cs = angles.at[TokenAngles<T, true>::place(k * (VecTraits<T>::kVec / 2) + i)];
-    const uint64_t c = ptx::pack2(cs.x, cs.y), s = ptx::pack2(cs.z, cs.w), minus = ptx::pack2(-cs.z, -cs.w);
-    out_lo = ptx::fma2(x, c, ptx::mul2(y, minus));
-    out_hi = ptx::fma2(y, c, ptx::mul2(x, s));
+    return weight ? to_float(reinterpret_cast<const T*>(weight)[channel]) : 1.f;
+}
+
+// Channels 2 i, 2 i + 1 of a head's vectors lo, hi (vector k of the half), times inv and the weights, turned.
+template <typename T>
+__device__ __forceinline__ void norm_turn_pair(const TokenAngles<T, true>& angles, int k, int i, float inv, const uint4& lo, const uint4& hi, uint64_t& out_lo,
+                                               uint64_t& out_hi)
+{
+    const uint64_t inv2 = ptx::pack2(inv, inv), x = ptx::mul2(pair_of<T>(lo, i), inv2), y = ptx::mul2(pair_of<T>(hi, i), inv2);
+    const float4* a = angles.at + TokenAngles<T, true>::place(k * (VecTraits<T>::kVec / 2) + i);
+    const float4 f = a[0], g = a[1];
+    out_lo = ptx::fma2(x, ptx::pack2(f.x, f.y), ptx::mul2(y, ptx::pack2(f.z, f.w)));
+    out_hi = ptx::fma2(y, ptx::pack2(g.x, g.y), ptx::mul2(x, ptx::pack2(g.z, g.w)));
 }
 
 // The heads of a token, by the lanes of one or several warps: work items it, it + step, ... of its items (pairs of vectors of query heads, of key
 // heads from q_items on, vectors of value heads from qk_items on; step is a multiple of 32, so a lane's place k in a head stays).  prepare() fills
-// the angles, while the first item's vectors are on their way, and returns the token's row in the cache; the next item's are requested
+// the angles (NORM: two sets, with the queries' weights and with the keys'), while the first item's vectors are on their way, and returns the token's row in the cache; the next item's are requested
 // before an item is worked on.  All lanes of the warp call this.
 template <typename T, bool NORM, typename F>
-__device__ __forceinline__ void token_heads(const RopeArgs& a, const NormArgs& nrm, const TokenAngles<T, NORM>& angles, int tok, int it, int step, int q_items,
+__device__ __forceinline__ void token_heads(const RopeArgs& a, const NormArgs& nrm, const TokenAngles<T, NORM>* angles, int tok, int it, int step, int q_items,
                                             int qk_items, int items, long kv_rows, F&& prepare)
 {
     constexpr int V = VecTraits<T>::kVec;
@@ -128,9 +133,8 @@ __device__ __forceinline__ void token_heads(const RopeArgs& a, const NormArgs& n
             r0 = *reinterpret_cast<const uint4*>(v + (i - qk_items) * V);
         }
     };
-    uint4 n0, n1, w0 = make_uint4(0u, 0u, 0u, 0u), w1 = w0;
+    uint4 n0, n1;
     load(it, n0, n1);
-    const T* held = nullptr;                       // whose weights w0, w1 are
     const long row = prepare();
     T* q_rot = (T*)a.q_rot + (long)tok * a.G * D + k * V;
     T* k_to = (T*)a.k_cache + row * D + k * V;
@@ -143,24 +147,16 @@ __device__ __forceinline__ void token_heads(const RopeArgs& a, const NormArgs& n
             const bool is_q = it < q_items;
             uint4 y0, y1;
             if constexpr (NORM) {
-                const T* weight = (const T*)(is_q ? nrm.q_weight : nrm.k_weight);
-                if (weight != held) {
-                    held = weight;
-                    if (weight) {
-                        w0 = *reinterpret_cast<const uint4*>(weight + k * V);
-                        w1 = *reinterpret_cast<const uint4*>(weight + k * V + half);
-                    }
-                }
                 const float inv = norm_factor<T>(r0, r1, vph, D, nrm.eps);
 #pragma unroll
                 for (int i = 0; i < V / 2; ++i) {
                     uint64_t lo, hi;
-                    norm_turn_pair<T>(angles, k, i, inv, weight != nullptr, w0, w1, r0, r1, lo, hi);
+                    norm_turn_pair<T>(angles[is_q ? 0 : 1], k, i, inv, r0, r1, lo, hi);
                     set_pair<T>(y0, i, lo);
                     set_pair<T>(y1, i, hi);
                 }
             } else {
-                Rotation<T>::turn(angles.at, k, r0, r1, y0, y1);
+                Rotation<T>::turn(angles->at, k, r0, r1, y0, y1);
             }
             if (it < qk_items) {
                 const int h = (is_q ? it : it - q_items) >> vph, g = (int)fast_div((uint32_t)h, a.div_g);
@@ -176,15 +172,35 @@ __device__ __forceinline__ void token_heads(const RopeArgs& a, const NormArgs& n
     }
 }
 
-// Fills a token's angles by the lanes of a warp; omega: of angle lane and, D = 128, lane + 32 (without a table).
-template <bool TABLE, typename Angles>
-__device__ __forceinline__ void fill_angles(Angles& s, const RopeArgs& a, int pos, const double (&omega)[2])
+// Fills a token's angles by the lanes of a warp (the sets that it needs); omega: of angle lane and, D = 128, lane + 32 (without a table).
+template <typename T, bool NORM, bool TABLE>
+__device__ __forceinline__ void fill_angles(TokenAngles<T, NORM>* s, const RopeArgs& a, const NormArgs& nrm, int pos, const double (&omega)[2], bool for_q, bool for_k)
 {
-    const int half = a.D / 2, lane = threadIdx.x & 31;
+    const int half = a.D / 2, lane = threadIdx.x & 31, last = half - 1;         // (a lane without a second angle reads another one's)
+    double2 cs[2];
+    float wq[2][2], wk[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (TABLE) cs[i] = a.table[(long)(pos - a.table_first) * half + min(lane + 32 * i, last)];
+    if (NORM) {                                    // in flight together with the table's
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int channel = min(lane + 32 * (i & 1), last) + half * (i >> 1);
+            if (for_q) wq[i & 1][i >> 1] = weight_of<T>(nrm.q_weight, channel);
+            if (for_k) wk[i & 1][i >> 1] = weight_of<T>(nrm.k_weight, channel);
+        }
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int j = lane + 32 * i;
-        if (j < half) s.put(j, TABLE ? a.table[(long)(pos - a.table_first) * half + j] : rope_cos_sin_at(pos, omega[i]));
+        if (j >= half) break;
+        if (!TABLE) cs[i] = rope_cos_sin_at(pos, omega[i]);
+        if constexpr (NORM) {
+            if (for_q) s[0].put(j, cs[i], wq[i][0], wq[i][1]);
+            if (for_k) s[1].put(j, cs[i], wk[i][0], wk[i][1]);
+        } else {
+            s->put(j, cs[i]);
+        }
     }
     __syncwarp();
 }
@@ -206,7 +222,7 @@ __global__ void __launch_bounds__(32 * kNormWarps, kNormBlocks)
 norm_append_kernel(const RopeArgs a, const NormArgs nrm, int token_warps, FastDiv div_warps, const __grid_constant__ LensT lens)
 {
     constexpr int V = VecTraits<T>::kVec;
-    __shared__ __align__(16) TokenAngles<T, true> s_angles[kNormWarps];
+    __shared__ __align__(16) TokenAngles<T, true> s_angles[kNormWarps][2];
     const int D = a.D, vph = a.vph_shift, wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int w = blockIdx.x * kNormWarps + wid, tok = (int)fast_div((uint32_t)w, div_warps), part = w - tok * token_warps;
     if (tok >= a.num_new) {
@@ -237,7 +253,8 @@ norm_append_kernel(const RopeArgs a, const NormArgs nrm, int token_warps, FastDi
         }
         const int pos = PAGED ? lens.cache_len[b] + tok - lens.new_off[b] : a.cache_len + tok;
         const long row = PAGED ? (long)a.page_table[(long)b * a.max_pages + (pos >> a.page_shift)] * a.Hkv * a.page_size + (pos & (a.page_size - 1)) : pos;
-        fill_angles<TABLE>(s_angles[wid], a, pos, omega);
+        const int first = 32 * part, step = 32 * token_warps;     // (several rounds: the keys' come in one of them)
+        if (first < qk_items) fill_angles<T, true, TABLE>(s_angles[wid], a, nrm, pos, omega, first < q_items, first + 32 > q_items || first + step < qk_items);
         return row;
     });
 }
