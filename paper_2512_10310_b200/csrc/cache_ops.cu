@@ -136,8 +136,8 @@ evlnStatus_t launch_norm_append(evlnHandle_t h, const RopeArgs& a, const evlnHea
 void batch_lens(BatchLens* bl, const evlnPagedParams* p, const int* lens, const int* offs)
 {
     memset(bl, 0, sizeof(*bl));
-    for (int b = 0; b < p->batch; ++b) bl->cache_len[b] = lens[b];
-    for (int b = 0; b <= kMaxBatch; ++b) bl->new_off[b] = offs[b < p->batch ? b : p->batch];
+    memcpy(bl->cache_len, lens, (size_t)p->batch * sizeof(int));
+    memcpy(bl->new_off, offs, ((size_t)p->batch + 1) * sizeof(int));
 }
 
 // ---- attention over the cache in 8 bits ----------------------------------------------------------
@@ -295,7 +295,7 @@ evlnStatus_t evlnPaged8RopeAppend(evlnHandle_t h, const evlnPagedParams* p, cons
     BatchLens bl;
     batch_lens(&bl, p, h_cache_lens, h_new_offsets);
     long pages = 0;
-    for (int b = 0; b <= kMaxBatch; ++b) {
+    for (int b = 0; b <= p->batch; ++b) {
         bl.item_off[b] = (int)pages;
         if (b >= p->batch) continue;
         const int L = h_cache_lens[b], n = h_new_offsets[b + 1] - h_new_offsets[b];
@@ -356,7 +356,7 @@ evlnStatus_t evlnPaged8StepAttention(evlnHandle_t h, const evlnPagedParams* p, c
     if (pl.expand) {
         const evlnPagedParams c = copy_params(p, pl);
         int at = 0;
-        for (int b = 0; b <= kMaxBatch; ++b) {
+        for (int b = 0; b <= p->batch; ++b) {
             bl.item_off[b] = at;
             if (b < p->batch && h_new_offsets[b + 1] > h_new_offsets[b]) at += ceil_div(h_cache_lens[b] + h_new_offsets[b + 1] - h_new_offsets[b], kPage8);
         }
@@ -376,7 +376,7 @@ evlnStatus_t evlnPaged8StepAttention(evlnHandle_t h, const evlnPagedParams* p, c
     }
 
     int at = 0;
-    for (int b = 0; b <= kMaxBatch; ++b) {
+    for (int b = 0; b <= p->batch; ++b) {
         bl.item_off[b] = at;
         if (b >= p->batch) continue;
         const int L = h_cache_lens[b], n = h_new_offsets[b + 1] - h_new_offsets[b];
