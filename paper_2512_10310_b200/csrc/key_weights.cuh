@@ -12,7 +12,9 @@
 // Bound: many rows, the special-function unit (16 exponentials a cycle and SM; the products take a quarter of that); few
 // rows, reading the keys once.  (1372 rows of 4 kv heads over 4292 keys: 13.4 us, 5 of them exponentials; over 20196 46.4.  Two groups that fetched their
 // log-sum-exps themselves, and masked every block of a tile that some row does not see, took 15.3 and 58.8: a wait that has to poll costs 0.1 us,
-// a fetch 0.3 us.  Chunks of 64 rows are bound by the issuing warp, 17.9.)
+// a fetch 0.3 us.  Chunks of 64 rows are bound by the issuing warp, 17.9, of 256 have too few buffers, 14.5; a quarter to a half of the exponentials on the
+// FMA pipe, by a polynomial of degree 5: 13.9 to 14.4.  Per SM sub-partition, 32 scores of 32 keys take 360 cycles: 256 of exponentials, beside
+// loads from tensor memory and products that alone take 340.)
 // Few tiles: the chunks of a tile are dealt to the CTAs of a cluster, whose sums meet in the first one's shared memory, in order.
 // fp32: a thread per key with its row in registers, query rows broadcast from shared memory, float FMAs.
 #pragma once
