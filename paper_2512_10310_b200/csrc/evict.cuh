@@ -85,8 +85,8 @@ select_keys_kernel(const SelectArgs a)
     uint32_t prefix = 0;
     int left = a.open;                                    // still to be found among the keys with this prefix
     if (search) {
-        // the keys, and their first digits: four loads in flight
-        constexpr int kBatch = 4;
+        // the keys, and their first digits: eight loads in flight
+        constexpr int kBatch = 8;
         for (int base = from + tid; base < to; base += kBatch * kSelectThreads) {
             float x[kBatch];
 #pragma unroll
