@@ -16,7 +16,7 @@
 // FMA pipe, by a polynomial of degree 5: 13.9 to 14.4.  Per SM sub-partition, 32 scores of 32 keys take 360 cycles: 256 of exponentials, beside
 // loads from tensor memory and products that alone take 340.)
 // Few tiles: the chunks of a tile are dealt to the CTAs of a cluster, whose sums meet in the first one's shared memory, in order.
-// fp32: a thread per key with its row in registers, query rows broadcast from shared memory, float FMAs.
+// fp32: a thread per key with its row in registers, query rows broadcast from shared memory, float FMAs; or 8 keys x 8 rows a thread.
 #pragma once
 
 #include <cuda.h>
@@ -381,6 +381,109 @@ key_weights_f32_kernel(const KeyWeightArgs a)
         if (rank > 0) return;
         for (int r = 1; r < csize; ++r) sum += s_remote[r][threadIdx.x];
     }
+    if (key < total) a.out[(long)g * a.cap + key] = (key < a.L ? a.in[(long)g * a.cap + key] * a.decay : 0.f) + sum;
+}
+
+// ---- fp32, many rows and keys: a matrix product in registers ---------------------------------
+// A thread of the kernel above loads four numbers of a query row for four FMAs, and the loads bind (448 rows of 4 heads over 4096 keys 121 us,
+// 15.8 TFLOP/s).  Here a thread owns 8 keys and 8 rows, whose vectors come out of shared memory four channels at a time: 256 FMAs for 16 loads (84 us:
+// now latency, two blocks of four warps an SM).  A warp: 128 keys x 16 rows; a block: a tile of keys, 64 rows at a time.
+constexpr int kKwTileRows = 64, kKwTileLeastRows = 32;
+template <int D>
+struct KwTilePlan {
+    static constexpr int kRow = D + 4;                    // floats between rows: eight lanes' 16 bytes start in different banks
+    static constexpr int kQOff = kTileN * kRow, kLseOff = kQOff + kKwTileRows * kRow, kSumOff = kLseOff + kKwTileRows;      // floats
+    static constexpr int kRemoteOff = kSumOff + 4 * kTileN, kBytes = (kRemoteOff + kKwMaxCluster * kTileN) * 4;
+};
+
+template <int D>
+__global__ void __launch_bounds__(128, 2)
+key_weights_tile_kernel(const KeyWeightArgs a)
+{
+    using Plan = KwTilePlan<D>;
+    constexpr int ROW = Plan::kRow, V = D / 4;
+    extern __shared__ __align__(16) float s_all[];
+    float* s_q = s_all + Plan::kQOff;
+    float* s_lse = s_all + Plan::kLseOff;
+    float* s_sum = s_all + Plan::kSumOff;
+    float* s_remote = s_all + Plan::kRemoteOff;
+    const int csize = (int)gridDim.y, rank = (int)blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int t = (int)fast_div(blockIdx.x, a.div_hkv), g = (int)blockIdx.x - t * a.Hkv;
+    const int key0 = t * kTileN, total = a.L + a.n;
+    if (csize > 1) ptx::cluster_arrive_relaxed();
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
+    for (int e = tid; e < kTileN * V; e += 128) {
+        const int r = e / V, c = e % V;
+        const float4* row = reinterpret_cast<const float4*>((const float*)a.k_cache + ((long)g * a.cap + min(key0 + r, total - 1)) * D);
+        *reinterpret_cast<float4*>(s_all + r * ROW + 4 * c) = row[c];
+    }
+    const int kl = lane & 15, my_row = warp * 16 + (lane >> 4) * 8;        // the thread's keys: kl + 16 j, rows my_row + i
+    float sums[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[j] = 0.f;
+    for (int c = first_chunk(a, key0) + rank; c < a.chunks; c += csize) {
+        const int row0 = c * kKwTileRows;
+        __syncthreads();
+        for (int e = tid; e < kKwTileRows * V; e += 128) {
+            const int r = e / V, d = e % V;
+            const float4* row = reinterpret_cast<const float4*>((const float*)a.q_rot + ((long)g * a.rows + row0 + r) * D);
+            *reinterpret_cast<float4*>(s_q + r * ROW + 4 * d) = row0 + r < a.rows ? row[d] : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        if (tid < kKwTileRows && row0 + tid < a.rows) {
+            const int r = row0 + tid, i = (int)fast_div((uint32_t)r, a.div_g);
+            s_lse[tid] = a.lse[(long)i * (a.Hkv * a.G) + g * a.G + (r - i * a.G)] * 1.4426950408889634f;
+        }
+        __syncthreads();
+        if (row0 + warp * 16 >= a.rows) continue;         // (whole warps; the barriers above are reached by all)
+        float s[8][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[i][j] = 0.f;
+#pragma unroll 1
+        for (int d = 0; d < D; d += 4) {
+            float4 k[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) k[j] = *reinterpret_cast<const float4*>(s_all + (kl + 16 * j) * ROW + d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float4 q = *reinterpret_cast<const float4*>(s_q + (my_row + i) * ROW + d);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[i][j] = fmaf(q.x, k[j].x, fmaf(q.y, k[j].y, fmaf(q.z, k[j].z, fmaf(q.w, k[j].w, s[i][j]))));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = row0 + my_row + i;
+            const float l = s_lse[my_row + i];
+            if (r >= a.rows) continue;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int key = key0 + kl + 16 * j;       // row r sees keys up to L + r / G
+                if (r >= max(key - a.L, 0) * a.G) sums[j] += exp2f(fmaf(s[i][j], a.scale_log2, -l));
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        sums[j] += __shfl_xor_sync(0xffffffffu, sums[j], 16);
+        if (lane < 16) s_sum[warp * kTileN + kl + 16 * j] = sums[j];
+    }
+    __syncthreads();
+    float sum = (s_sum[tid] + s_sum[kTileN + tid]) + (s_sum[2 * kTileN + tid] + s_sum[3 * kTileN + tid]);
+    if (csize > 1) {
+        ptx::cluster_wait();
+        if (rank > 0) {
+            const uint32_t to = ptx::map_to_cta(ptx::smem_u32(s_remote + rank * kTileN + tid), 0);
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(sum) : "memory");
+        }
+        ptx::cluster_arrive();
+        ptx::cluster_wait();
+        if (rank > 0) return;
+        for (int r = 1; r < csize; ++r) sum += s_remote[r * kTileN + tid];
+    }
+    const int key = key0 + tid;
     if (key < total) a.out[(long)g * a.cap + key] = (key < a.L ? a.in[(long)g * a.cap + key] * a.decay : 0.f) + sum;
 }
 

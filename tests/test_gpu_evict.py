@@ -57,6 +57,9 @@ def _weights_case(dtype, hq, hkv, D, L, n, cap, seed, scale):
     ("f32", 28, 4, 128, 300, 7, 1.0, 0.0),
     ("f32", 3, 3, 128, 0, 1, 1.0, 0.0),
     ("f32", 4, 2, 64, 1000, 130, 0.0, 0.2),
+    ("f32", 28, 4, 128, 4096, 5, 1.0, 0.0),         # 35 rows as tiles of keys and rows
+    ("f32", 64, 8, 128, 2000, 50, 0.9, 0.0),        # ... several chunks, the last one short, a tile that only some rows see
+    ("f32", 12, 1, 128, 15000, 30, 1.0, 0.0),
 ])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_key_weights(handle, dtype, hq, hkv, D, L, n, decay, scale, in_place):
