@@ -436,14 +436,14 @@ evlnStatus_t evlnKeyWeights(evlnHandle_t h, const evlnStepParams* p, const void*
     a.div_hkv = make_fast_div((uint32_t)a.Hkv);
     const bool f32 = p->dtype == EVLN_F32;
     // fp32, both sides in us (28/4 heads of 128): 28 rows over 4096 keys 16.8 a thread per key, 17.3 as tiles; 56 rows 29.4 and 18.3, over 9000 46.3 and 24.6;
-    // 448 rows over 4096 121 and 84, but over 3000, which leave a third of the SMs without a tile, 196 rows 34.6 and 48.2.  Heads of 64 gain nothing (9000
+    // 448 rows over 4096 121 and 78, but over 3000, which leave a third of the SMs without a tile, 196 rows 34.6 and 48.2.  Heads of 64 gain nothing (9000
     // keys, 196 rows 48.3 and 56.3): their keys leave room for more warps.
     const bool tile = f32 && D == 128 && a.rows > kKwTileLeastRows && 4L * a.items >= 3L * h->num_sms;
     a.chunk_rows = tile ? kKwTileRows : f32 ? kKwF32Rows : a.rows >= kKwRows ? kKwRows : (a.rows + 31) / 32 * 32;
     a.chunks = ceil_div(a.rows, a.chunk_rows);
-    // few tiles: a cluster of CTAs for each, as many as the SMs (fp32: four blocks an SM) and the chunks allow
+    // few tiles: a cluster of CTAs for each, as many as the SMs (fp32: four blocks an SM, two of tiles) and the chunks allow
     int cluster = 1;
-    while (cluster < kKwMaxCluster && 2 * cluster <= a.chunks && 2L * cluster * a.items <= (f32 ? 4L : 1L) * h->num_sms) cluster *= 2;
+    while (cluster < kKwMaxCluster && 2 * cluster <= a.chunks && 2L * cluster * a.items <= (tile ? 2L : f32 ? 4L : 1L) * h->num_sms) cluster *= 2;
     const dim3 grid((unsigned)(cluster > 1 || f32 || a.items < h->num_sms ? a.items : h->num_sms), (unsigned)cluster);
     cudaStream_t st = (cudaStream_t)stream;
     if (tile)

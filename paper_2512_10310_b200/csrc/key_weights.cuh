@@ -386,7 +386,7 @@ key_weights_f32_kernel(const KeyWeightArgs a)
 
 // ---- fp32, many rows and keys: a matrix product in registers ---------------------------------
 // A thread of the kernel above loads four numbers of a query row for four FMAs, and the loads bind (448 rows of 4 heads over 4096 keys 121 us,
-// 15.8 TFLOP/s).  Here a thread owns 8 keys and 8 rows, whose vectors come out of shared memory four channels at a time: 256 FMAs for 16 loads (84 us:
+// 15.8 TFLOP/s).  Here a thread owns 8 keys and 8 rows, whose vectors come out of shared memory four channels at a time: 256 FMAs for 16 loads (78 us:
 // now latency, two blocks of four warps an SM).  A warp: 128 keys x 16 rows; a block: a tile of keys, 64 rows at a time.
 constexpr int kKwTileRows = 64, kKwTileLeastRows = 32;
 template <int D>
