@@ -321,7 +321,9 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                 float keep[NQ];
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
-                    const float f = factor[q] * ks;                   // > 0
+                    // > 0 and finite: zeros times it stay zeros and masked scores -inf (a page of zero keys has the scale 2^-120, which
+                    // small queries' factor would take below the least float)
+                    const float f = fminf(fmaxf(factor[q] * ks, 0x1p-126f), 0x1p127f);
                     float top = -INFINITY;
 #pragma unroll
                     for (int t = 0; t < 4; ++t) top = ptx::max3(top, sc[t][2 * q], sc[t][2 * q + 1]);
