@@ -7,9 +7,10 @@
 // (cvt f16x2 <- e4m3x2, exact), and everything else that the format asks for is free or done once per row:
 //  - the query row is scaled by a power of two into the range of halves (exact above 2^-29 of the row's maximum), and that
 //    factor, the page's key scale and the softmax scale are one factor on the scores;
-//  - the page's value scale, a power of two, goes into the exponent of the probabilities: p' = 2^(s - m + log2(scale / r)),
-//    r the largest value scale that the warp has met; the row sums take it out again.  (Probabilities are rounded to halves:
-//    2^-11, finer than bf16.)
+//  - the page's value scale 2^v goes into the exponent of the probabilities: p' = 2^(s + v - (m + r)), r a number of the row that keeps
+//    p' between the ends of the halves; the row sums, of 2^(s - m), take it out again.  A row's r follows the largest product of probability and
+//    value scale that it has met, not the largest scale: pages that the row gives no weight do not move it, however large their values.
+//    (p' is rounded to halves: 2^-11 of itself, finer than bf16, or 2^-31 of the row's largest p * scale.)
 // The operands come out of ldmatrix as bytes: a key's 16 bytes are a k-step of the score product (four channels a lane, the
 // queries are laid out the same way), and a transposed load of byte PAIRS gives two keys of two neighbouring channels,
 // which one byte permutation parts.  The second product is transposed, O^T = V^T P^T: what the scores leave in a lane's registers is
@@ -22,7 +23,7 @@
 // to the warps in turn, which joins all of them at the end of every unit, took 45 us for 16 ragged episodes of a token, runs 38.)
 // Runs are equally long, KG of them per SM; a unit that the runs cut across blocks leaves parts, which merge8_kernel
 // joins.  The lanes of a warp look 32 stages ahead for page numbers and scales (a lane each).
-// A row's reference m follows its maximum only when that is 2^8 above it, so outputs are rarely scaled anew.
+// A row's references m and m + r follow the maxima of s and s + v only when those are 2^8 above them, so outputs are rarely scaled anew.
 #pragma once
 
 #include <cuda.h>
@@ -38,7 +39,7 @@ constexpr int kA8Keys = 32, kA8StageBytes = 2 * kA8Keys * 128;
 constexpr int kA8OStride = 132;                       // floats between rows of the joint's buffers (every second one starts 8 banks on)
 constexpr float kA8Headroom = 8.f;                    // p' <= 2^(headroom + lift), below the largest half
 constexpr int kA8Lift = 6;
-constexpr int kA8LeastRatio = -40;                    // log2 of the smallest value-scale ratio that is told apart (halves end at -24 - lift)
+constexpr float kA8LeastGap = -90.f;                  // least v - r that is told apart: below it p' is 0 as a half, and its float is still what the sum needs
 
 template <int NQ, int RG>
 struct Attn8Plan {
@@ -48,7 +49,7 @@ struct Attn8Plan {
     static constexpr int kRegs = 168;
     static constexpr int kWarpRows = 8 * NQ, kRows = kWarpRows * RG;
     static constexpr int kKeyGroups = kWarps / RG;
-    static constexpr int kStatBytes = kWarps * kWarpRows * 8 + 128;            // references and sums; value scales of the runs, the units that they ended in
+    static constexpr int kStatBytes = kWarps * kWarpRows * 16 + 128;           // references and sums; the units that the runs ended in
     static constexpr int kBarBytes = 512;
     static constexpr int kRest = kStatBytes + kBarBytes + 1024;
     static constexpr int kFit = (227 * 1024 - kRest) / kA8StageBytes / kKeyGroups;
@@ -71,7 +72,7 @@ struct Attn8Args {
     __nv_bfloat16* out;              // [tokens, Hq, 128]
     float* lse_out;                  // [tokens, Hq] or null
     float* o_part;                   // [2 * runs, rows of a block, 128]
-    float2* ml_part;                 // [2 * runs, rows of a block]: reference (log2) and sum
+    float4* ml_part;                 // [2 * runs, rows of a block]: m (log2), sum in units of 2^m, r: o_part is in units of 2^(m + r - lift)
     int* status;
     int Hkv, G, rows, batch, max_pages;
     int run, total;                  // stages of a run, of the batch
@@ -106,6 +107,8 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// 2^e of a whole number e between -126 and 127 that is held as a float
+__device__ __forceinline__ float exp2_whole(float e) { return __uint_as_float(__float_as_uint(8388608.f + 127.f + e) << 23); }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
 {
     uint32_t r;
@@ -130,6 +133,11 @@ __device__ __forceinline__ long out_row8(const Attn8Args& a, const BatchLens& le
 }
 constexpr float kLn2 = 0.69314718055994531f;
 
+// Parts of a row with references m and m + r, joined at top and top + joint_r: the largest m, and about the largest m + r (`high`), so that no part's
+// outputs leave the range of floats.  (-inf: no part has a key of the row.)
+__device__ __forceinline__ float joint_base(float top) { return top == -INFINITY ? 0.f : top; }
+__device__ __forceinline__ float joint_r(float top, float high) { return top == -INFINITY ? 0.f : fminf(fmaxf(high - top, -120.f), 120.f); }
+
 template <int NQ, int RG>
 __global__ void __launch_bounds__(Attn8Plan<NQ, RG>::kThreads) __maxnreg__((Attn8Plan<NQ, RG>::kRegs))
 attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Attn8Args a, const __grid_constant__ BatchLens lens)
@@ -139,9 +147,8 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
-    float2* s_ml = reinterpret_cast<float2*>(smem_gen + Plan::kStatOff);           // [KG][ROWS]
-    float* s_scale = reinterpret_cast<float*>(s_ml + KG * ROWS);                   // [KG]
-    int* s_unit = reinterpret_cast<int*>(s_scale + KG);                            // [KG] first stage of the unit that the run ended in, -1: nothing left
+    float4* s_ml = reinterpret_cast<float4*>(smem_gen + Plan::kStatOff);           // [KG][ROWS] as ml_part
+    int* s_unit = reinterpret_cast<int*>(s_ml + KG * ROWS);                        // [KG] first stage of the unit that the run ended in, -1: nothing left
     volatile int* s_abort = reinterpret_cast<volatile int*>(smem_gen + Plan::kBarOff + 16 * KG * SLOTS);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = lane & 3, lrow = lane >> 2;
@@ -246,9 +253,9 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     bool ok = true;
     int i = 0, slot = 0;                               // the run's next stage
     uint32_t parity = 0;
-    // o: transposed, [8-row tile][16 channels 16 c ..]: channels 16 c + 2 lrow (first two) and + 1, rows 2 quad and 2 quad + 1 of the tile; m, l: rows lrow
-    float o[NQ][8][4], m[NQ], l[NQ];
-    int ref = 0;                                       // the largest value scale so far, as the float's exponent field; 0: none
+    // o: transposed, [8-row tile][16 channels 16 c ..]: channels 16 c + 2 lrow (first two) and + 1, rows 2 quad and 2 quad + 1 of the tile; m, l, r: rows
+    // lrow (r: a whole number)
+    float o[NQ][8][4], m[NQ], l[NQ], r[NQ];
     bool left = false;                                 // the unit at hand goes to the joint
     while (i < mine) {
         if (i > 0) {
@@ -262,14 +269,13 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         int last[NQ];                                  // the row's last key
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-            const int r = q * 8 + lrow;
-            last[q] = row0 + r < rows_here ? u.L + (int)fast_div((uint32_t)(row0 + r), a.div_g) : u.L + u.n - 1;
+            const int row = row0 + q * 8 + lrow;
+            last[q] = row < rows_here ? u.L + (int)fast_div((uint32_t)row, a.div_g) : u.L + u.n - 1;
 #pragma unroll
             for (int c = 0; c < 8; ++c) o[q][c][0] = o[q][c][1] = o[q][c][2] = o[q][c][3] = 0.f;
             m[q] = -INFINITY;
-            l[q] = 0.f;
+            l[q] = r[q] = 0.f;
         }
-        ref = 0;
 
         for (; r0 + i < end; ++i) {
             if ((i & 31) == 0 && i > 0) {
@@ -301,13 +307,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                     }
                 }
                 // ---- softmax: references, probabilities, sums ----
-                const int own = (int)(__float_as_uint(vs) >> 23);     // (a power of two; uniform over the warp)
-                const bool grew = own > ref;
-                const float shrink = !grew ? 1.f : own - ref > 100 ? 0.f : exp2_int(ref - own);
-                bool moved = grew && ref > 0;
-                if (grew) ref = own;
-                const int steps = max(own - ref, kA8LeastRatio) + kA8Lift;
-                const float ratio = (float)steps, unlift = exp2_int(-steps);
+                const float v = (float)((int)(__float_as_uint(vs) >> 23) - 127);      // (a power of two; uniform over the warp)
                 if (key0 + kA8Keys - 1 > u.L) {                       // keys that not every row sees
 #pragma unroll
                     for (int q = 0; q < NQ; ++q)
@@ -317,26 +317,46 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                             for (int e = 0; e < 2; ++e)
                                 if (key0 + 8 * t + 2 * quad + e > last[q]) sc[t][2 * q + e] = -INFINITY;
                 }
-                uint32_t p[NQ][2][2];                                 // the transposed product's operand: two k-steps of 16 keys
-                float keep[NQ];
+                float f[NQ], top[NQ];
+                bool move[NQ], moved = false;
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
                     // > 0 and finite: zeros times it stay zeros and masked scores -inf (a page of zero keys has the scale 2^-120, which
                     // small queries' factor would take below the least float)
-                    const float f = fminf(fmaxf(factor[q] * ks, 0x1p-126f), 0x1p127f);
-                    float top = -INFINITY;
+                    f[q] = fminf(fmaxf(factor[q] * ks, 0x1p-126f), 0x1p127f);
+                    top[q] = -INFINITY;
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) top = ptx::max3(top, sc[t][2 * q], sc[t][2 * q + 1]);
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * f;
-                    const bool move = top > m[q] + kA8Headroom;       // (from -inf: whenever there is a score)
-                    const float was = m[q];
-                    if (move) m[q] = top;
-                    const float alpha = move ? ptx::ex2(was - top) : 1.f;
-                    keep[q] = alpha * shrink;
-                    moved = moved || move;
-                    const float off = ratio - (m[q] == -INFINITY ? 0.f : m[q]);
-                    const uint64_t f2 = ptx::pack2(f, f), off2 = ptx::pack2(off, off);
+                    for (int t = 0; t < 4; ++t) top[q] = ptx::max3(top[q], sc[t][2 * q], sc[t][2 * q + 1]);
+                    top[q] = fmaxf(top[q], __shfl_xor_sync(0xffffffffu, top[q], 1));
+                    top[q] = fmaxf(top[q], __shfl_xor_sync(0xffffffffu, top[q], 2)) * f[q];
+                    move[q] = top[q] + fmaxf(v - r[q], 0.f) > m[q] + kA8Headroom;     // (from -inf: whenever there is a score)
+                    moved = moved || move[q];
+                }
+                if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                    for (int q = 0; q < NQ; ++q) {
+                        float keep = 1.f;
+                        if (move[q]) {
+                            // m + r as it was or as this page wants it, whichever is larger; rounded down, so that it does not creep up
+                            const float to = fmaxf(m[q], top[q]), back = m[q] - to, r_to = floorf(fmaxf(r[q] + back, v + (top[q] - to)));
+                            l[q] *= ptx::ex2(back);
+                            keep = ptx::ex2(back + (r[q] - r_to));
+                            m[q] = to;
+                            r[q] = r_to;
+                        }
+                        const float k0 = __shfl_sync(0xffffffffu, keep, 8 * quad), k1 = __shfl_sync(0xffffffffu, keep, 8 * quad + 4);   // rows 2 quad, 2 quad + 1
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            o[q][c][0] *= k0; o[q][c][1] *= k1;
+                            o[q][c][2] *= k0; o[q][c][3] *= k1;
+                        }
+                    }
+                }
+                uint32_t p[NQ][2][2];                                 // the transposed product's operand: two k-steps of 16 keys
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) {
+                    const float steps = fmaxf(v - r[q], kA8LeastGap) + (float)kA8Lift, off = steps - (m[q] == -INFINITY ? 0.f : m[q]);
+                    const uint64_t f2 = ptx::pack2(f[q], f[q]), off2 = ptx::pack2(off, off);
                     uint64_t sum2 = 0;
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
@@ -349,18 +369,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                     }
                     float x, y;
                     ptx::unpack2(sum2, x, y);
-                    l[q] = fmaf(l[q], alpha, (x + y) * unlift);
-                }
-                if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-                    for (int q = 0; q < NQ; ++q) {
-                        const float k0 = __shfl_sync(0xffffffffu, keep[q], 8 * quad), k1 = __shfl_sync(0xffffffffu, keep[q], 8 * quad + 4);   // rows 2 quad, 2 quad + 1
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            o[q][c][0] *= k0; o[q][c][1] *= k1;
-                            o[q][c][2] *= k0; o[q][c][3] *= k1;
-                        }
-                    }
+                    l[q] = fmaf(x + y, exp2_whole(fmaxf(-steps, -126.f)), l[q]);
                 }
                 // ---- products with the values, transposed: 16 channels down, 8 rows across ----
 #pragma unroll
@@ -403,23 +412,25 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         if (!left) {
 #pragma unroll
             for (int q = 0; q < NQ; ++q) {
-                const float value = __uint_as_float((uint32_t)(ref - kA8Lift) << 23), by_row = !whole ? value : l[q] == 0.f ? 0.f : value / l[q];
+                const float by_row = l[q] == 0.f ? 0.f : 1.f / l[q], value = exp2_whole(r[q] - (float)kA8Lift);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int from = 8 * quad + 4 * e;
-                    const float by = __shfl_sync(0xffffffffu, by_row, from), mr = __shfl_sync(0xffffffffu, m[q], from), lr = __shfl_sync(0xffffffffu, l[q], from);
-                    const int r = q * 8 + 2 * quad + e;
-                    if (row0 + r >= rows_here) continue;
+                    const float by = __shfl_sync(0xffffffffu, by_row, from), scale = __shfl_sync(0xffffffffu, value, from);
+                    const float mr = __shfl_sync(0xffffffffu, m[q], from), lr = __shfl_sync(0xffffffffu, l[q], from), rr = __shfl_sync(0xffffffffu, r[q], from);
+                    const int row = q * 8 + 2 * quad + e;
+                    if (row0 + row >= rows_here) continue;
                     if (whole) {
-                        const long at = out_row8(a, lens, u, row0 + r);
+                        const long at = out_row8(a, lens, u, row0 + row);
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) reinterpret_cast<uint32_t*>(a.out + at * 128)[8 * c + lrow] = ptx::pack_bf16x2(o[q][c][e] * by, o[q][c][2 + e] * by);
+                        for (int c = 0; c < 8; ++c)
+                            reinterpret_cast<uint32_t*>(a.out + at * 128)[8 * c + lrow] = ptx::pack_bf16x2(o[q][c][e] * by * scale, o[q][c][2 + e] * by * scale);
                         if (a.lse_out && lrow == 0) a.lse_out[at] = (mr + log2f(lr)) * kLn2;
                     } else {
-                        const long at = 2L * run * ROWS + row0 + r;
+                        const long at = 2L * run * ROWS + row0 + row;
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) reinterpret_cast<float2*>(a.o_part + at * 128)[8 * c + lrow] = make_float2(o[q][c][e] * by, o[q][c][2 + e] * by);
-                        if (lrow == 0) a.ml_part[at] = make_float2(mr, lr);
+                        for (int c = 0; c < 8; ++c) reinterpret_cast<float2*>(a.o_part + at * 128)[8 * c + lrow] = make_float2(o[q][c][e], o[q][c][2 + e]);
+                        if (lrow == 0) a.ml_part[at] = make_float4(mr, lr, rr, 0.f);
                     }
                 }
             }
@@ -432,7 +443,6 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     else __syncwarp();
     if (rg == 0 && lane == 0) {
         s_unit[kg] = left ? u.first : -1;
-        s_scale[kg] = __uint_as_float((uint32_t)(ref - kA8Lift) << 23);
     }
     if (left) {
         float* to = reinterpret_cast<float*>(smem_gen + kg * SLOTS * kA8StageBytes) + (rg * WROWS + 2 * quad) * kA8OStride + 2 * lrow;
@@ -442,7 +452,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int c = 0; c < 8; ++c) *reinterpret_cast<float2*>(to + (q * 8 + e) * kA8OStride + 16 * c) = make_float2(o[q][c][e], o[q][c][2 + e]);
-            if (quad == 0) s_ml[kg * ROWS + rg * WROWS + q * 8 + lrow] = make_float2(m[q], l[q]);
+            if (quad == 0) s_ml[kg * ROWS + rg * WROWS + q * 8 + lrow] = make_float4(m[q], l[q], r[q], 0.f);
         }
     }
     __syncthreads();
@@ -462,33 +472,35 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             const bool whole = first_run * a.run <= w.first && ends == w.first + w.stages;
             const int rows_here = w.n * a.G;
 #pragma unroll 1
-            for (int r = warp; r < rows_here; r += Plan::kWarps) {                   // a warp per row, four channels a lane
-                float2 ml[KG];
-                float4 y[KG];
-                float top = -INFINITY, sum = 0.f;
+            for (int row = warp; row < rows_here; row += Plan::kWarps) {             // a warp per row, four channels a lane
+                float4 ml[KG], y[KG];
+                float top = -INFINITY, high = -INFINITY, sum = 0.f;                 // of m, of m + r
 #pragma unroll
                 for (int k = 0; k < KG; ++k) {
                     const bool in = k >= k0 && k < k1;
-                    ml[k] = in ? s_ml[k * ROWS + r] : make_float2(-INFINITY, 0.f);
-                    y[k] = in ? *reinterpret_cast<const float4*>(smem_gen + k * SLOTS * kA8StageBytes + (r * kA8OStride + 4 * lane) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    ml[k] = in ? s_ml[k * ROWS + row] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+                    y[k] = in ? *reinterpret_cast<const float4*>(smem_gen + k * SLOTS * kA8StageBytes + (row * kA8OStride + 4 * lane) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
                     top = fmaxf(top, ml[k].x);
+                    high = fmaxf(high, ml[k].x + ml[k].z);
                 }
+                const float base = joint_base(top), r_to = joint_r(top, high);
                 float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int k = 0; k < KG; ++k) {
-                    const float by = ml[k].x == -INFINITY ? 0.f : ptx::ex2(ml[k].x - top), f = by * s_scale[k];
-                    sum = fmaf(ml[k].y, by, sum);
+                    const float back = ml[k].x - base, f = ptx::ex2(back + (ml[k].z - r_to));
+                    sum = fmaf(ml[k].y, ptx::ex2(back), sum);
                     x.x = fmaf(y[k].x, f, x.x); x.y = fmaf(y[k].y, f, x.y); x.z = fmaf(y[k].z, f, x.z); x.w = fmaf(y[k].w, f, x.w);
                 }
                 if (whole) {
-                    const long at = out_row8(a, lens, w, r);
-                    const float by = sum == 0.f ? 0.f : 1.f / sum;
-                    reinterpret_cast<uint2*>(a.out + at * 128)[lane] = make_uint2(ptx::pack_bf16x2(x.x * by, x.y * by), ptx::pack_bf16x2(x.z * by, x.w * by));
+                    const long at = out_row8(a, lens, w, row);
+                    const float by = sum == 0.f ? 0.f : 1.f / sum, scale = ptx::ex2(r_to - (float)kA8Lift);
+                    reinterpret_cast<uint2*>(a.out + at * 128)[lane] =
+                        make_uint2(ptx::pack_bf16x2(x.x * by * scale, x.y * by * scale), ptx::pack_bf16x2(x.z * by * scale, x.w * by * scale));
                     if (a.lse_out && lane == 0) a.lse_out[at] = (top + log2f(sum)) * kLn2;
                 } else {
-                    const long at = (2L * first_run + 1) * ROWS + r;
+                    const long at = (2L * first_run + 1) * ROWS + row;
                     reinterpret_cast<float4*>(a.o_part + at * 128)[lane] = x;
-                    if (lane == 0) a.ml_part[at] = make_float2(top, sum);
+                    if (lane == 0) a.ml_part[at] = make_float4(top, sum, r_to, 0.f);
                 }
             }
         }
@@ -549,13 +561,11 @@ merge8_kernel(const Attn8Args a, const __grid_constant__ BatchLens lens, const _
         const int b0 = ra / KG, joints = (on ? rb - 1 : rb) / KG - b0 + 1, parts = joints + (on ? 1 : 0);
         auto row_of = [&](int p, int r) -> long { return (p < joints ? 2L * max(ra, (b0 + p) * KG) + 1 : 2L * rb) * ROWS + r; };
         for (int r = blockIdx.y; r < u.n * a.G; r += gridDim.y) {
-            float4 y[kMergeAhead];
-            float2 ml[kMergeAhead];
+            float4 y[kMergeAhead], ml[kMergeAhead];
             auto fetch = [&](int p0) {
 #pragma unroll
                 for (int i = 0; i < kMergeAhead; ++i) {
                     const int p = p0 + WARPS * i;
-                    ml[i] = make_float2(-INFINITY, 0.f);
                     if (p < parts) {
                         const long at = row_of(p, r);
                         y[i] = reinterpret_cast<const float4*>(a.o_part + at * 128)[lane];
@@ -564,18 +574,26 @@ merge8_kernel(const Attn8Args a, const __grid_constant__ BatchLens lens, const _
                 }
             };
             fetch(warp);
-            float top = -INFINITY, sum = 0.f;
-            for (int p = lane; p < parts; p += 32) top = fmaxf(top, a.ml_part[row_of(p, r)].x);
+            float top = -INFINITY, high = -INFINITY, sum = 0.f;      // of m, of m + r
+            for (int p = lane; p < parts; p += 32) {
+                const float4 of = a.ml_part[row_of(p, r)];
+                top = fmaxf(top, of.x);
+                high = fmaxf(high, of.x + of.z);
+            }
 #pragma unroll
-            for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+            for (int s = 16; s > 0; s >>= 1) {
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+                high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, s));
+            }
+            const float base = joint_base(top), r_to = joint_r(top, high);
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
             for (int p0 = warp;;) {
 #pragma unroll
                 for (int i = 0; i < kMergeAhead; ++i) {
                     if (p0 + WARPS * i >= parts) break;
-                    const float w = ml[i].x == -INFINITY ? 0.f : ptx::ex2(ml[i].x - top);      // -inf: no key of the row in this part
-                    sum = fmaf(ml[i].y, w, sum);
+                    const float back = ml[i].x - base, w = ptx::ex2(back + (ml[i].z - r_to));      // -inf: no key of the row in this part
+                    sum = fmaf(ml[i].y, ptx::ex2(back), sum);
                     x.x = fmaf(y[i].x, w, x.x); x.y = fmaf(y[i].y, w, x.y); x.z = fmaf(y[i].z, w, x.z); x.w = fmaf(y[i].w, w, x.w);
                 }
                 p0 += WARPS * kMergeAhead;
@@ -594,9 +612,9 @@ merge8_kernel(const Attn8Args a, const __grid_constant__ BatchLens lens, const _
                     z.x += part.x; z.y += part.y;
                     sum += s_sum[w];
                 }
-                const float by = 1.f / sum;
+                const float by = 1.f / sum, scale = ptx::ex2(r_to - (float)kA8Lift);
                 const long at = out_row8(a, lens, u, r);
-                reinterpret_cast<uint32_t*>(a.out + at * 128)[threadIdx.x] = ptx::pack_bf16x2(z.x * by, z.y * by);
+                reinterpret_cast<uint32_t*>(a.out + at * 128)[threadIdx.x] = ptx::pack_bf16x2(z.x * by * scale, z.y * by * scale);
                 if (a.lse_out && threadIdx.x == 0) a.lse_out[at] = (top + log2f(sum)) * kLn2;
             }
             __syncthreads();

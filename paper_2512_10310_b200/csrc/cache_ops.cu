@@ -193,7 +193,7 @@ evlnStatus_t plan8(evlnHandle_t h, const evlnPagedParams* p, const int* lens, co
     return EVLN_OK;
 }
 
-size_t part_bytes8(const Plan8& pl) { return round_up((size_t)2 * pl.runs * pl.rows * (128 + 2) * sizeof(float), 256); }
+size_t part_bytes8(const Plan8& pl) { return round_up((size_t)2 * pl.runs * pl.rows * (128 + 4) * sizeof(float), 256); }
 
 // The paged call that serves the bf16 copy.
 evlnPagedParams copy_params(const evlnPagedParams* p, const Plan8& pl)
@@ -395,7 +395,7 @@ evlnStatus_t evlnPaged8StepAttention(evlnHandle_t h, const evlnPagedParams* p, c
     a.page_table = d_page_table;
     a.out = (__nv_bfloat16*)out; a.lse_out = lse_out;
     a.o_part = (float*)workspace;
-    a.ml_part = (float2*)(a.o_part + (size_t)2 * pl.runs * pl.rows * 128);
+    a.ml_part = (float4*)(a.o_part + (size_t)2 * pl.runs * pl.rows * 128);
     a.status = h->d_status;
     a.Hkv = hkv; a.G = G; a.rows = total * G; a.batch = p->batch; a.max_pages = p->max_pages_per_seq;
     a.run = pl.run; a.total = pl.total;
