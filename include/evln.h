@@ -421,8 +421,10 @@ evlnStatus_t evlnStoreFetch(evlnHandle_t handle, const evlnGatherParams* params,
  *
  * evlnRopeAppend / evlnPagedRopeAppend with a norm of every query and key head in the same pass:
  *     y = w * x / sqrt(mean(x^2) + eps)        mean over the D channels of the head,
- * then the rotation, then the stores.  Sums are fp32, and there is one rounding, to the storage type, after the rotation
- * (none between norm and rotation).  Values are copied.  A head of zeros with eps = 0 gives NaN, as the formula does.
+ * then the rotation, then the stores.  There is one rounding to the storage type, after the rotation (none between norm and
+ * rotation).  What comes before it is formed in double for f32, as by evlnRopeAppend, and in fp32 for bf16 (angles in double, then
+ * rounded to fp32): a head whose squares leave the range of floats (|x| of 2^60, or below 2^-60 with eps = 0) is not normalised
+ * there.  Values are copied.  A head of zeros with eps = 0 gives NaN, as the formula does.
  * A model whose weights are stored as w - 1 passes 1 + them.  The paged call takes token strides, as the contiguous one
  * does, so that q, k and v may be views of one projection's rows.                                        */
 typedef struct {

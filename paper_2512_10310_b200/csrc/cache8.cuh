@@ -172,9 +172,9 @@ append8_kernel(const Append8Args p, const __grid_constant__ BatchLens lens)
                 s_angles.of_slots[wid][i / 2].put(j, TABLE ? a.table[(long)(pos - a.table_first) * half + j] : rope_cos_sin(pos, j, D, a.log2_theta), w[i & 1][0], w[i & 1][1]);
         }
         __syncwarp();
-        const float inv = NORM ? norm_factor<T>(r0[u], r1[u], 3, D, p.norm.eps) : 1.f;
+        const float inv = NORM ? NormFactor<T>::of(r0[u], r1[u], 3, D, p.norm.eps) : 1.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) norm_turn_pair<T>(s_angles.of_slots[wid][slot0 & 3], k, i, inv, r0[u], r1[u], x[u][0][i], x[u][1][i]);
+        for (int i = 0; i < 4; ++i) norm_turn_pair(s_angles.of_slots[wid][slot0 & 3], k, i, inv, r0[u], r1[u], x[u][0][i], x[u][1][i]);
     }
     // the page's maximum; infinities and NaN do not count (an infinity becomes the largest code, NaN a NaN code)
     float most = 0.f;

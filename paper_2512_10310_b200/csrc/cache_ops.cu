@@ -124,7 +124,7 @@ template <typename T, bool PAGED, typename LensT>
 evlnStatus_t launch_norm_append(evlnHandle_t h, const RopeArgs& a, const evlnHeadNorm* norm, int extra, const LensT& lens, void* stream)
 {
     const int items = ((a.Hq + a.Hkv) << a.vph_shift) + (a.Hkv << (a.vph_shift + 1));
-    const int warps = token_warps(a.num_new, items, (long)h->num_sms * kNormWarps * kNormBlocks - extra);
+    const int warps = token_warps(a.num_new, items, (long)h->num_sms * kNormWarps * kNormBlocks<T> - extra);
     const long blocks = ((long)a.num_new * warps + extra + kNormWarps - 1) / kNormWarps;
     if (blocks > 0x7fffffL) return EVLN_NOT_SUPPORTED;
     auto launch = [&](auto kernel) {

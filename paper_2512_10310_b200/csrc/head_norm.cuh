@@ -4,8 +4,8 @@
 //
 // then the rotation of Sec. 3.2 at the token's position and the stores of rope_append.cuh.  A head vector is 2^s lanes of
 // one warp, a pair of 16-byte vectors (channels j.. and j + D/2..) each: the sum of squares is V packed FMAs and s
-// shuffles, and the pair is what the rotation wants.  Everything after the load is in floats (two channels an instruction) and rounded once,
-// to the storage type: there is no rounding between norm and rotation, as there is where they are two passes.
+// shuffles, and the pair is what the rotation wants.  Everything after the load is in floats (two channels an instruction; fp32: in double, as the
+// rotation without norms) and rounded once, to the storage type: there is no rounding between norm and rotation, as there is where they are two passes.
 // A warp serves one token: it fills the token's angles, the weights multiplied into them, into its own corner of shared memory, then takes 32 work items
 // after the other, so that no warp waits for another one and the angles' cost is shared.  As many warps per token as are resident together: a second
 // wave costs more than a longer loop (392 tokens of 28 + 8 heads: 9 warps each 4.1 us, 10 warps and two waves 6.2).
@@ -22,7 +22,10 @@ namespace evln {
 
 // A block: four warps (of eight, the first of few tokens started later: 1.9 us for a token, 1.5).  Seven blocks an SM leave a thread 72 registers, which the
 // loop fits (392 tokens 4.2 us, 4.3 with six blocks, 3136 13.9 with both; eight blocks and 64 registers 15.8: the compiler puts some of it aside).
-constexpr int kNormWarps = 4, kNormBlocks = 7;
+// In fp32 a thread holds doubles: four blocks an SM.  (28/4 heads: a token 1.7 us, 392 tokens 5.6, 3136 33.7, in floats 1.6, 4.8 and 23.9 with errors of
+// 700 roundings where the products cancel: conversions to double and back bind.)
+constexpr int kNormWarps = 4;
+template <typename T> constexpr int kNormBlocks = sizeof(T) == 4 ? 4 : 7;
 
 struct NormArgs {
     const void* q_weight;    // [D] of the tokens' type, or null: ones
@@ -55,27 +58,53 @@ __device__ __forceinline__ void set_pair<__nv_bfloat16>(uint4& raw, int i, uint6
 }
 
 // 1 / sqrt(mean square + eps) of a head vector that 2^shift neighbouring lanes hold, lo and hi each (all lanes of the warp call this).  D: 2^n.
-template <typename T>
-__device__ __forceinline__ float norm_factor(const uint4& lo, const uint4& hi, int shift, int D, float eps)
-{
-    uint64_t ss2 = 0;
+template <typename T> struct NormFactor;
+template <> struct NormFactor<__nv_bfloat16> {
+    typedef float F;
+    static __device__ __forceinline__ F of(const uint4& lo, const uint4& hi, int shift, int D, float eps)
+    {
+        uint64_t ss2 = 0;
 #pragma unroll
-    for (int i = 0; i < VecTraits<T>::kVec / 2; ++i) {
-        const uint64_t x = pair_of<T>(lo, i), y = pair_of<T>(hi, i);
-        ss2 = ptx::fma2(x, x, ptx::fma2(y, y, ss2));
+        for (int i = 0; i < 4; ++i) {
+            const uint64_t x = pair_of<__nv_bfloat16>(lo, i), y = pair_of<__nv_bfloat16>(hi, i);
+            ss2 = ptx::fma2(x, x, ptx::fma2(y, y, ss2));
+        }
+        float ss, other;
+        ptx::unpack2(ss2, ss, other);
+        ss += other;
+        for (int s = 0; s < shift; ++s) ss += __shfl_xor_sync(0xffffffffu, ss, 1 << s);
+        return rsqrtf(fmaf(ss, 1.f / (float)D, eps));
     }
-    float ss, other;
-    ptx::unpack2(ss2, ss, other);
-    ss += other;
-    for (int s = 0; s < shift; ++s) ss += __shfl_xor_sync(0xffffffffu, ss, 1 << s);
-    return rsqrtf(fmaf(ss, 1.f / (float)D, eps));
-}
+};
+template <> struct NormFactor<float> {
+    typedef double F;
+    static __device__ __forceinline__ F of(const uint4& lo, const uint4& hi, int shift, int D, float eps)
+    {
+        const float* x = reinterpret_cast<const float*>(&lo);
+        const float* y = reinterpret_cast<const float*>(&hi);
+        double ss = 0.0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ss = fma((double)x[i], (double)x[i], fma((double)y[i], (double)y[i], ss));
+        for (int s = 0; s < shift; ++s) ss += __shfl_xor_sync(0xffffffffu, ss, 1 << s);
+        return rsqrt(fma(ss, 1.0 / (double)D, (double)eps));
+    }
+};
 
-// A token's D/2 angles in shared memory.  NORM: with the weights w of a head's channels j and j + D/2 in them, for two channels (c w_j, -s w_j'; c w_j',
-// s w_j), the eight vectors of eight channels to 144 bytes, so that the lanes of a head start in different banks; else as the rotation of
-// a stored number wants them.
+// A token's D/2 angles in shared memory.  NORM: with the weights w of a head's channels j and j + D/2 in them, (c w_j, -s w_j'; c w_j', s w_j), bf16 for
+// two channels side by side; the vectors of a head (eight channels, fp32 four) 144 bytes apart, so that its lanes start in different banks.  Else as the
+// rotation of a stored number wants them.
 template <typename T, bool NORM> struct TokenAngles;
-template <typename T> struct TokenAngles<T, true> {
+template <> struct TokenAngles<float, true> {
+    double2 at[144];
+    static __device__ __forceinline__ int place(int j) { return 9 * (j >> 2) + 2 * (j & 3); }
+    __device__ __forceinline__ void put(int j, const double2& cs, float lo, float hi)
+    {
+        double2* to = at + place(j);
+        to[0] = make_double2(cs.x * lo, -(cs.y * hi));
+        to[1] = make_double2(cs.x * hi, cs.y * lo);
+    }
+};
+template <> struct TokenAngles<__nv_bfloat16, true> {
     float4 at[72];
     static __device__ __forceinline__ int place(int pair) { return 9 * (pair >> 2) + 2 * (pair & 3); }
     __device__ __forceinline__ void put(int j, const double2& cs, float lo, float hi)
@@ -99,15 +128,30 @@ __device__ __forceinline__ float weight_of(const void* weight, int channel)
 }
 
 // Channels 2 i, 2 i + 1 of a head's vectors lo, hi (vector k of the half), times inv and the weights, turned.
-template <typename T>
-__device__ __forceinline__ void norm_turn_pair(const TokenAngles<T, true>& angles, int k, int i, float inv, const uint4& lo, const uint4& hi, uint64_t& out_lo,
-                                               uint64_t& out_hi)
+__device__ __forceinline__ void norm_turn_pair(const TokenAngles<__nv_bfloat16, true>& angles, int k, int i, float inv, const uint4& lo, const uint4& hi,
+                                               uint64_t& out_lo, uint64_t& out_hi)
 {
+    typedef __nv_bfloat16 T;
     const uint64_t inv2 = ptx::pack2(inv, inv), x = ptx::mul2(pair_of<T>(lo, i), inv2), y = ptx::mul2(pair_of<T>(hi, i), inv2);
-    const float4* a = angles.at + TokenAngles<T, true>::place(k * (VecTraits<T>::kVec / 2) + i);
+    const float4* a = angles.at + TokenAngles<T, true>::place(4 * k + i);
     const float4 f = a[0], g = a[1];
     out_lo = ptx::fma2(x, ptx::pack2(f.x, f.y), ptx::mul2(y, ptx::pack2(f.z, f.w)));
     out_hi = ptx::fma2(y, ptx::pack2(g.x, g.y), ptx::mul2(x, ptx::pack2(g.z, g.w)));
+}
+__device__ __forceinline__ void norm_turn_pair(const TokenAngles<float, true>& angles, int k, int i, double inv, const uint4& lo, const uint4& hi,
+                                               uint64_t& out_lo, uint64_t& out_hi)
+{
+    float to_lo[2], to_hi[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const double x = (double)reinterpret_cast<const float*>(&lo)[2 * i + e] * inv, y = (double)reinterpret_cast<const float*>(&hi)[2 * i + e] * inv;
+        const double2* a = angles.at + TokenAngles<float, true>::place(4 * k + 2 * i + e);
+        const double2 f = a[0], g = a[1];
+        to_lo[e] = (float)fma(x, f.x, y * f.y);
+        to_hi[e] = (float)fma(y, g.x, x * g.y);
+    }
+    out_lo = ptx::pack2(to_lo[0], to_lo[1]);
+    out_hi = ptx::pack2(to_hi[0], to_hi[1]);
 }
 
 // The heads of a token, by the lanes of one or several warps: work items it, it + step, ... of its items (pairs of vectors of query heads, of key
@@ -147,11 +191,11 @@ __device__ __forceinline__ void token_heads(const RopeArgs& a, const NormArgs& n
             const bool is_q = it < q_items;
             uint4 y0, y1;
             if constexpr (NORM) {
-                const float inv = norm_factor<T>(r0, r1, vph, D, nrm.eps);
+                const typename NormFactor<T>::F inv = NormFactor<T>::of(r0, r1, vph, D, nrm.eps);
 #pragma unroll
                 for (int i = 0; i < V / 2; ++i) {
                     uint64_t lo, hi;
-                    norm_turn_pair<T>(angles[is_q ? 0 : 1], k, i, inv, r0, r1, lo, hi);
+                    norm_turn_pair(angles[is_q ? 0 : 1], k, i, inv, r0, r1, lo, hi);
                     set_pair<T>(y0, i, lo);
                     set_pair<T>(y1, i, hi);
                 }
@@ -218,7 +262,7 @@ __device__ __forceinline__ void own_omegas(const RopeArgs& a, double (&omega)[2]
 // token_warps warps per new token, each with every token_warps-th 32 of its items; PAGED: then one per episode and head that clears the value
 // slots behind the episode's last token.
 template <typename T, bool PAGED, bool TABLE, typename LensT>
-__global__ void __launch_bounds__(32 * kNormWarps, kNormBlocks)
+__global__ void __launch_bounds__(32 * kNormWarps, kNormBlocks<T>)
 norm_append_kernel(const RopeArgs a, const NormArgs nrm, int token_warps, FastDiv div_warps, const __grid_constant__ LensT lens)
 {
     constexpr int V = VecTraits<T>::kVec;
