@@ -19,7 +19,8 @@
  *    h_ (host memory, read during the call).  The library never allocates or frees in
  *    these calls and keeps no reference to caller memory after a call returns.
  *  - All device base pointers must be 16-byte aligned, token strides multiples of 8
- *    elements (bf16) / 4 elements (f32); otherwise EVLN_INVALID_VALUE.
+ *    elements (bf16) / 4 elements (f32); otherwise EVLN_INVALID_VALUE.  (Arrays of floats and ints,
+ *    such as log-sum-exps, page tables, scales, weights and slots: 4 bytes.)
  *  - Calls validate on the host, then enqueue kernels on `stream` (a cudaStream_t passed as
  *    void*; NULL = default stream) and return without synchronising.  Argument errors
  *    launch nothing.  EVLN_CUDA_ERROR wraps a failed launch; evlnGetLastCudaError gives

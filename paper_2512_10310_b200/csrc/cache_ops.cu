@@ -261,7 +261,7 @@ evlnStatus_t evlnPagedNormRopeAppend(evlnHandle_t h, const evlnPagedParams* p, c
     const void* pointers[6] = {q_new, k_new, v_new, q_rot, k_pool, v_pool};
     s = check_tokens(pointers, 6, p->num_q_heads, p->num_kv_heads, 128, 8, q_stride_tok, k_stride_tok, v_stride_tok);
     if (s != EVLN_OK) return s;
-    if (!d_page_table || !device_is_current(h)) return EVLN_INVALID_VALUE;
+    if (!d_page_table || !aligned4(d_page_table) || !device_is_current(h)) return EVLN_INVALID_VALUE;
     RopeArgs a = token_args(p->num_q_heads, p->num_kv_heads, 128, 8, q_new, k_new, v_new, q_stride_tok, k_stride_tok, v_stride_tok, p->rope_theta, p->rope_table,
                             p->rope_table_first_pos);
     a.q_rot = q_rot; a.k_cache = k_pool; a.v_cache = v_pool; a.page_table = d_page_table;
@@ -285,7 +285,7 @@ evlnStatus_t evlnPaged8RopeAppend(evlnHandle_t h, const evlnPagedParams* p, cons
     const void* pointers[6] = {q_new, k_new, v_new, q_rot, k_pool, v_pool};
     s = check_tokens(pointers, 6, p->num_q_heads, p->num_kv_heads, 128, 8, q_stride_tok, k_stride_tok, v_stride_tok);
     if (s != EVLN_OK) return s;
-    if (!d_page_table || !k_scale || !v_scale || !device_is_current(h)) return EVLN_INVALID_VALUE;
+    if (!d_page_table || !k_scale || !v_scale || !aligned4(d_page_table, k_scale, v_scale) || !device_is_current(h)) return EVLN_INVALID_VALUE;
     Append8Args a = {};
     a.r = token_args(p->num_q_heads, p->num_kv_heads, 128, 8, q_new, k_new, v_new, q_stride_tok, k_stride_tok, v_stride_tok, p->rope_theta, p->rope_table,
                      p->rope_table_first_pos);
@@ -344,7 +344,7 @@ evlnStatus_t evlnPaged8StepAttention(evlnHandle_t h, const evlnPagedParams* p, c
     const void* pointers[5] = {q_rot, k_pool, v_pool, workspace, out};
     for (const void* x : pointers)
         if (!x || !aligned16(x)) return EVLN_INVALID_VALUE;
-    if (!k_scale || !v_scale || !d_page_table || !device_is_current(h)) return EVLN_INVALID_VALUE;
+    if (!k_scale || !v_scale || !d_page_table || !aligned4(d_page_table, k_scale, v_scale, lse_out) || !device_is_current(h)) return EVLN_INVALID_VALUE;
     if (workspace_bytes < need) return EVLN_WORKSPACE_TOO_SMALL;
     Plan8 pl;
     s = plan8(h, p, h_cache_lens, h_new_offsets, &pl);
@@ -416,7 +416,8 @@ evlnStatus_t evlnKeyWeights(evlnHandle_t h, const evlnStepParams* p, const void*
     if (s != EVLN_OK) return s;
     if (!(decay >= 0.f)) return EVLN_INVALID_VALUE;
     if (p->num_new == 0) return EVLN_INVALID_VALUE;
-    if (!q_rot || !k_cache || !lse || !weights_in || !weights_out || !aligned16(q_rot) || !aligned16(k_cache)) return EVLN_INVALID_VALUE;
+    if (!q_rot || !k_cache || !lse || !weights_in || !weights_out || !aligned16(q_rot) || !aligned16(k_cache) || !aligned4(lse, weights_in, weights_out))
+        return EVLN_INVALID_VALUE;
     const size_t w_bytes = (size_t)p->num_kv_heads * p->cache_capacity * sizeof(float);
     if (weights_in != weights_out && overlap(weights_in, w_bytes, weights_out, w_bytes)) return EVLN_INVALID_VALUE;
     if (!device_is_current(h)) return EVLN_INVALID_VALUE;
@@ -473,7 +474,7 @@ evlnStatus_t evlnSelectKeys(evlnHandle_t h, const evlnGatherParams* p, const flo
     SelectArgs a = {};
     a.num_kept = budget < num_keys ? budget : num_keys;
     if (a.num_kept == 0) return EVLN_OK;
-    if (!weights || !kept) return EVLN_INVALID_VALUE;
+    if (!weights || !kept || !aligned4(weights, kept)) return EVLN_INVALID_VALUE;
     a.weights = weights; a.kept = kept;
     a.stride = p->store_capacity; a.num_keys = num_keys;
     a.sinks = sinks; a.recent = recent; a.open = budget - sinks - recent;
@@ -496,7 +497,7 @@ evlnStatus_t evlnGatherKeys(evlnHandle_t h, const evlnGatherParams* p, int num_k
     const void* pointers[4] = {k_store, v_store, k_work, v_work};
     for (const void* x : pointers)
         if (!x || !aligned16(x)) return EVLN_INVALID_VALUE;
-    if (!kept || (weights == nullptr) != (weights_work == nullptr)) return EVLN_INVALID_VALUE;
+    if (!kept || !aligned4(kept, weights, weights_work) || (weights == nullptr) != (weights_work == nullptr)) return EVLN_INVALID_VALUE;
     if (rotate && !rope_table_covers(p->rope_table, p->rope_table_first_pos, p->rope_table_count, 0, num_kept)) return EVLN_INVALID_VALUE;
     const size_t row = (size_t)p->num_kv_heads * p->head_dim * elem_bytes(p->dtype), src = row * p->store_capacity, dst = row * p->work_capacity;
     for (int i = 0; i < 2; ++i)

@@ -49,6 +49,12 @@ cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t s
 }
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// Arrays of floats and ints (null: one that the call may go without).
+template <typename... P>
+bool aligned4(const P*... p)
+{
+    return (((reinterpret_cast<uintptr_t>(p) & 3u) == 0) && ...);
+}
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
 {

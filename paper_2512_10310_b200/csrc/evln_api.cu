@@ -1365,7 +1365,7 @@ evlnStatus_t evlnStepCombine(evlnHandle_t h, const evlnStepParams* p, const void
     evlnStatus_t s = check_step_params(h, p);
     if (s != EVLN_OK) return s;
     if (p->num_new == 0) return EVLN_OK;
-    if (!workspace || !out || !aligned16(workspace) || !aligned16(out)) return EVLN_INVALID_VALUE;
+    if (!workspace || !out || !aligned16(workspace) || !aligned16(out) || !aligned4(lse_out)) return EVLN_INVALID_VALUE;
     if (!device_is_current(h)) return EVLN_INVALID_VALUE;
     const int G = p->num_q_heads / p->num_kv_heads;
     const int R = p->num_new * G;
@@ -1401,7 +1401,7 @@ evlnStatus_t evlnStep(evlnHandle_t h, const evlnStepParams* p, const void* q_new
     if (s != EVLN_OK) return s;
     if (p->num_new == 0) return EVLN_OK;
     // every argument is checked before the first launch, so a rejected call has done nothing
-    if (!workspace || !out || !aligned16(workspace) || !aligned16(out)) return EVLN_INVALID_VALUE;
+    if (!workspace || !out || !aligned16(workspace) || !aligned16(out) || !aligned4(lse_out)) return EVLN_INVALID_VALUE;
     const long rows = (long)p->num_new * (p->num_q_heads / p->num_kv_heads);
     if (workspace_bytes < partial_bytes(resolve_splits(h, p), p->num_kv_heads, rows, p->head_dim))
         return EVLN_WORKSPACE_TOO_SMALL;
@@ -1471,7 +1471,7 @@ evlnStatus_t evlnPagedRopeAppend(evlnHandle_t h, const evlnPagedParams* p, const
     if (total == 0) return EVLN_OK;
     if (!q_new || !k_new || !v_new || !d_page_table || !q_rot || !k_pool || !v_pool) return EVLN_INVALID_VALUE;
     if (!aligned16(q_new) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_rot) ||
-        !aligned16(k_pool) || !aligned16(v_pool))
+        !aligned16(k_pool) || !aligned16(v_pool) || !aligned4(d_page_table))
         return EVLN_INVALID_VALUE;
     if (!device_is_current(h)) return EVLN_INVALID_VALUE;
     RopeArgs a = {};
@@ -1502,7 +1502,7 @@ static evlnStatus_t paged_attention(evlnHandle_t h, const evlnPagedParams* p, co
     const int total = h_new_offsets[p->batch];
     if (total == 0) return EVLN_OK;
     if (!q_rot || !k_pool || !v_pool || !d_page_table || !workspace) return EVLN_INVALID_VALUE;
-    if (!aligned16(q_rot) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(workspace))
+    if (!aligned16(q_rot) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(workspace) || !aligned4(d_page_table))
         return EVLN_INVALID_VALUE;
     if (!device_is_current(h)) return EVLN_INVALID_VALUE;
     const int G = p->num_q_heads / p->num_kv_heads;
@@ -1632,7 +1632,7 @@ evlnStatus_t evlnPagedStepCombine(evlnHandle_t h, const evlnPagedParams* p, cons
     if (s != EVLN_OK) return s;
     const int total = h_new_offsets[p->batch];
     if (total == 0) return EVLN_OK;
-    if (!workspace || !out || !aligned16(workspace) || !aligned16(out)) return EVLN_INVALID_VALUE;
+    if (!workspace || !out || !aligned16(workspace) || !aligned16(out) || !aligned4(lse_out)) return EVLN_INVALID_VALUE;
     if (!device_is_current(h)) return EVLN_INVALID_VALUE;
     const int G = p->num_q_heads / p->num_kv_heads;
     const long rows = (long)total * G;
@@ -1765,7 +1765,7 @@ extern "C" evlnStatus_t evlnPackedForward(evlnHandle_t h, const evlnPackedParams
     if (pl.n_vis + pl.n_act == 0) return EVLN_OK;
     if (!q || !k || !v || !k_cache || !v_cache || !workspace || !out) return EVLN_INVALID_VALUE;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache) ||
-        !aligned16(workspace) || !aligned16(out))
+        !aligned16(workspace) || !aligned16(out) || !aligned4(lse_out))
         return EVLN_INVALID_VALUE;
     if (q_stride_tok < (long)p->num_q_heads * 128 || k_stride_tok < (long)p->num_kv_heads * 128 ||
         v_stride_tok < (long)p->num_kv_heads * 128 || q_stride_tok % 8 || k_stride_tok % 8 || v_stride_tok % 8)
@@ -2111,7 +2111,7 @@ extern "C" evlnStatus_t evlnStepAttentionNoAlloc(const evlnStepParams* p, const 
         fitting.num_splits = simt_schedule(h, p, 0, fit).splits;
         p = &fitting;
     }
-    if (!out || !aligned16(out)) return EVLN_INVALID_VALUE;
+    if (!out || !aligned16(out) || !aligned4(lse_out)) return EVLN_INVALID_VALUE;
     DirectOut direct = {out, lse_out, false};
     s = step_attention(h, p, q_rot, k_cache, v_cache, d->scratch, (size_t)EVLN_NOALLOC_SCRATCH_BYTES, stream,
                        output_over_q_rot(p, q_rot, out, lse_out) ? nullptr : &direct);
