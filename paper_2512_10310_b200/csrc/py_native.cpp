@@ -90,7 +90,9 @@ bool as_int(PyObject* o, int* v)
     long l;
     if (!as_long(o, &l)) return false;
     *v = (int)l;
-    return true;
+    if (*v == l) return true;
+    PyErr_Format(PyExc_OverflowError, "%ld does not fit 32 bits", l);       // (cut to them it would be another number)
+    return false;
 }
 
 // Address of a tensor (or of anything with data_ptr()), None -> NULL; plain integers pass through.
