@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import cache_ops_oracle as co
 from paper_2512_10310_b200 import binding as B
 from tests.helpers import f64
 from tests.test_gpu_cache8 import D, DEV, LSE_ERROR, P, Batch
@@ -79,3 +80,28 @@ def test_a_step_of_zeros(handle, n, L):
     out, lse = x.attend(q_rot)
     assert bool((out == 0).all())
     assert np.abs(f64(lse) - np.log(np.arange(L + 1, L + n + 1))[:, None]).max() <= LSE_ERROR
+
+
+@pytest.mark.parametrize("n", TOKENS)
+@pytest.mark.parametrize("L", [0, 3, 30, 500])
+def test_log_sum_exps_of_flat_scores(handle, n, L):
+    """Scores of small products, whose log-sum-exps show what exponentials and sums lose: 2^-22 an exponential, a rounding for each of the reference, the
+    logarithm and the product (2^-24 of a number the size of the result)."""
+    x = Batch(handle, [L], [n], 14, 2, seed=L + n, kv_size=0.1)
+    x.fill_new()
+    q_rot = x.q_rot(0.05)
+    out, lse = x.attend(q_rot)
+    x.check(q_rot, out, lse)
+    q, k = f64(q_rot).reshape(2, -1, 7, D).transpose(1, 0, 2, 3).reshape(-1, 14, D), x.episode(0, 0)
+    ref = co.attention(q, k, np.zeros_like(k), L, D ** -0.5)[1]
+    reach = np.abs(q).sum(-1).max() * np.abs(k).max() * D ** -0.5
+    assert (np.abs(f64(lse) - ref) <= 2.0 ** -21 + 2.0 ** -22 * (reach + np.abs(ref))).all()
+
+
+def test_a_frame_beside_single_tokens(handle):
+    """One episode of more than 64 rows: the whole batch goes through the copy, single tokens and an idle episode too."""
+    x = Batch(handle, [900, 5, 64, 0, 333, 1000], [1, 1, 1, 1, 30, 0], 28, 4, seed=3)
+    x.fill_new()
+    q_rot = x.q_rot()
+    out, lse = x.attend(q_rot)
+    x.check(q_rot, out, lse)
