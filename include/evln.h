@@ -466,7 +466,8 @@ evlnStatus_t evlnPagedNormRopeAppend(evlnHandle_t handle, const evlnPagedParams*
  * of two, as evlnPaged8RopeAppend leaves them; other scales give undefined numbers), out and lse_out (may be NULL) as
  * from evlnPagedStepAttention + evlnPagedStepCombine.  Up to 64 query rows per kv head are read from the codes
  * themselves, more are served from a bf16 copy of the batch's pages in the workspace (exact: code * scale is a bf16
- * number), so that evlnPaged8WorkspaceSize is larger for those.                                            */
+ * number), so that evlnPaged8WorkspaceSize is larger for those.  out and lse_out must not lie over q_rot (EVLN_INVALID_VALUE),
+ * except out = q_rot with one new token in all or one kv head.                                               */
 evlnStatus_t evlnPaged8RopeAppend(evlnHandle_t handle, const evlnPagedParams* params, const evlnHeadNorm* norm,
                                   const void* q_new, const void* k_new, const void* v_new,
                                   long q_stride_tok, long k_stride_tok, long v_stride_tok,

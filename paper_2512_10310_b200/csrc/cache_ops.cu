@@ -345,6 +345,11 @@ evlnStatus_t evlnPaged8StepAttention(evlnHandle_t h, const evlnPagedParams* p, c
     for (const void* x : pointers)
         if (!x || !aligned16(x)) return EVLN_INVALID_VALUE;
     if (!k_scale || !v_scale || !d_page_table || !aligned4(d_page_table, k_scale, v_scale, lse_out) || !device_is_current(h)) return EVLN_INVALID_VALUE;
+    // Outputs are written while other blocks read queries: not over them, unless every row goes where its own query lies (the layouts of one
+    // token or one kv head are the same).
+    const size_t rows_all = (size_t)total * p->num_q_heads, q_bytes = rows_all * 128 * 2;
+    const bool in_place = out == q_rot && (total == 1 || p->num_kv_heads == 1);
+    if ((!in_place && overlap(out, q_bytes, q_rot, q_bytes)) || (lse_out && overlap(lse_out, rows_all * sizeof(float), q_rot, q_bytes))) return EVLN_INVALID_VALUE;
     if (workspace_bytes < need) return EVLN_WORKSPACE_TOO_SMALL;
     Plan8 pl;
     s = plan8(h, p, h_cache_lens, h_new_offsets, &pl);
