@@ -427,7 +427,8 @@ evlnStatus_t evlnStoreFetch(evlnHandle_t handle, const evlnGatherParams* params,
  * rounded to fp32): a head whose squares leave the range of floats (|x| of 2^60, or below 2^-60 with eps = 0) is not normalised
  * there.  Values are copied.  A head of zeros with eps = 0 gives NaN, as the formula does.
  * A model whose weights are stored as w - 1 passes 1 + them.  The paged call takes token strides, as the contiguous one
- * does, so that q, k and v may be views of one projection's rows.                                        */
+ * does, so that q, k and v may be views of one projection's rows.  q_rot must not lie over the new tokens (EVLN_INVALID_VALUE),
+ * except q_rot = q_new with one new token in all, or one kv head and no gaps between the tokens' queries.     */
 typedef struct {
     size_t struct_size;      /* sizeof(evlnHeadNorm)                                         */
     const void* q_weight;    /* [D], the tokens' type, 16-byte aligned; NULL: ones           */

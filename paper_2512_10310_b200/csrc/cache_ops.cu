@@ -88,6 +88,18 @@ evlnStatus_t check_tokens(const void* const* pointers, int count, int hq, int hk
     return EVLN_OK;
 }
 
+// Rotated queries must not lie over the new tokens, which other warps still read, unless every query goes where it lies (the layouts of one token,
+// or of one kv head without gaps between tokens, are the same).
+evlnStatus_t check_q_rot(const void* q_rot, long tokens, int hq, int hkv, int D, int bytes, const void* q, const void* k, const void* v, long qs, long ks, long vs)
+{
+    auto extent = [&](int heads, long stride) { return ((size_t)(tokens - 1) * stride + (size_t)heads * D) * bytes; };
+    const size_t size = (size_t)tokens * hq * D * bytes;
+    const bool in_place = q_rot == q && (tokens == 1 || (hkv == 1 && qs == (long)hq * D));
+    if ((!in_place && overlap(q_rot, size, q, extent(hq, qs))) || overlap(q_rot, size, k, extent(hkv, ks)) || overlap(q_rot, size, v, extent(hkv, vs)))
+        return EVLN_INVALID_VALUE;
+    return EVLN_OK;
+}
+
 RopeArgs token_args(int hq, int hkv, int D, int vec, const void* q, const void* k, const void* v, long qs, long ks, long vs, double theta, const void* table,
                     int table_first)
 {
@@ -239,6 +251,9 @@ evlnStatus_t evlnNormRopeAppend(evlnHandle_t h, const evlnStepParams* p, const e
     const int vec = 16 / elem_bytes(p->dtype);
     const void* pointers[6] = {q_new, k_new, v_new, q_rot, k_cache, v_cache};
     s = check_tokens(pointers, 6, p->num_q_heads, p->num_kv_heads, p->head_dim, vec, q_stride_tok, k_stride_tok, v_stride_tok);
+    if (s == EVLN_OK)
+        s = check_q_rot(q_rot, p->num_new, p->num_q_heads, p->num_kv_heads, p->head_dim, elem_bytes(p->dtype), q_new, k_new, v_new, q_stride_tok, k_stride_tok,
+                        v_stride_tok);
     if (s != EVLN_OK) return s;
     if (!device_is_current(h)) return EVLN_INVALID_VALUE;
     RopeArgs a = token_args(p->num_q_heads, p->num_kv_heads, p->head_dim, vec, q_new, k_new, v_new, q_stride_tok, k_stride_tok, v_stride_tok, p->rope_theta,
@@ -260,6 +275,8 @@ evlnStatus_t evlnPagedNormRopeAppend(evlnHandle_t h, const evlnPagedParams* p, c
     if (total == 0) return EVLN_OK;
     const void* pointers[6] = {q_new, k_new, v_new, q_rot, k_pool, v_pool};
     s = check_tokens(pointers, 6, p->num_q_heads, p->num_kv_heads, 128, 8, q_stride_tok, k_stride_tok, v_stride_tok);
+    if (s == EVLN_OK)
+        s = check_q_rot(q_rot, total, p->num_q_heads, p->num_kv_heads, 128, 2, q_new, k_new, v_new, q_stride_tok, k_stride_tok, v_stride_tok);
     if (s != EVLN_OK) return s;
     if (!d_page_table || !aligned4(d_page_table) || !device_is_current(h)) return EVLN_INVALID_VALUE;
     RopeArgs a = token_args(p->num_q_heads, p->num_kv_heads, 128, 8, q_new, k_new, v_new, q_stride_tok, k_stride_tok, v_stride_tok, p->rope_theta, p->rope_table,
@@ -284,6 +301,8 @@ evlnStatus_t evlnPaged8RopeAppend(evlnHandle_t h, const evlnPagedParams* p, cons
     if (total == 0) return EVLN_OK;
     const void* pointers[6] = {q_new, k_new, v_new, q_rot, k_pool, v_pool};
     s = check_tokens(pointers, 6, p->num_q_heads, p->num_kv_heads, 128, 8, q_stride_tok, k_stride_tok, v_stride_tok);
+    if (s == EVLN_OK)
+        s = check_q_rot(q_rot, total, p->num_q_heads, p->num_kv_heads, 128, 2, q_new, k_new, v_new, q_stride_tok, k_stride_tok, v_stride_tok);
     if (s != EVLN_OK) return s;
     if (!d_page_table || !k_scale || !v_scale || !aligned4(d_page_table, k_scale, v_scale) || !device_is_current(h)) return EVLN_INVALID_VALUE;
     Append8Args a = {};
