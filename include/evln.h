@@ -446,8 +446,9 @@ evlnStatus_t evlnPagedNormRopeAppend(evlnHandle_t handle, const evlnPagedParams*
                                      const int* h_cache_lens, const int* h_new_offsets, const int* d_page_table,
                                      void* q_rot, void* k_pool, void* v_pool, void* stream);
 
-/* ---- paged cache in 8 bits (no counterpart in the paper: half the bytes of the cache, so twice the episodes on a GPU
- *      and half the time of a step that is bound by reading it) --------------------------------------------------
+/* ---- paged cache in 8 bits (no counterpart in the paper: half the bytes of the cache, so twice the episodes on a GPU.
+ *      A step of up to 16 query rows per kv head, which reading the cache bounds, takes 0.6 to 0.95 of its time over the
+ *      paged bf16 cache, one of more than 32 rows 1.1 to 1.7 of it) ------------------------------------------------
  *
  * k_pool, v_pool [num_pages, Hkv, 64, 128] hold codes of one byte (e4m3: 4 exponent, 3 fraction bits, largest 448,
  * no infinities, NaN 0x7f / 0xff), k_scale, v_scale [num_pages, Hkv] a float for each page and kv head:
@@ -464,11 +465,15 @@ evlnStatus_t evlnPagedNormRopeAppend(evlnHandle_t handle, const evlnPagedParams*
  * cleared up to the end of its page; key slots there, and pages that no new token goes to, are left as they were.
  *
  * evlnPaged8StepAttention: causal attention of the rotated queries over such a cache (the scales of its pages are powers
- * of two, as evlnPaged8RopeAppend leaves them; other scales give undefined numbers), out and lse_out (may be NULL) as
- * from evlnPagedStepAttention + evlnPagedStepCombine.  Up to 64 query rows per kv head are read from the codes
- * themselves, more are served from a bf16 copy of the batch's pages in the workspace (exact: code * scale is a bf16
- * number), so that evlnPaged8WorkspaceSize is larger for those.  out and lse_out must not lie over q_rot (EVLN_INVALID_VALUE),
- * except out = q_rot with one new token in all or one kv head.                                               */
+ * of two, 2^-120 to 2^120, as evlnPaged8RopeAppend leaves them; other scales give undefined numbers), out and lse_out (may be
+ * NULL) as from evlnPagedStepAttention + evlnPagedStepCombine.  A batch whose episodes have up to 64 query rows per kv head each is
+ * served from the codes themselves; as soon as one has more, the whole batch is served from a bf16 copy of its pages in the
+ * workspace (exact: code * scale is a bf16 number), so that evlnPaged8WorkspaceSize is about twice the 8-bit cache and the call
+ * longer by the copy (28/4 heads, 15 single tokens and a frame 175 us, 16 single tokens 31: two calls are faster than one).
+ * Scores, sums and outputs are fp32; probabilities are rounded for the product with the values: on the codes to 2^-11 of
+ * themselves or 2^-31 of the row's largest product of probability and page scale, through the copy to 2^-8 of themselves.
+ * A NaN among the values of a step's new tokens may reach every row of its episode, as in the bf16 calls.
+ * out and lse_out must not lie over q_rot (EVLN_INVALID_VALUE), except out = q_rot with one new token in all or one kv head. */
 evlnStatus_t evlnPaged8RopeAppend(evlnHandle_t handle, const evlnPagedParams* params, const evlnHeadNorm* norm,
                                   const void* q_new, const void* k_new, const void* v_new,
                                   long q_stride_tok, long k_stride_tok, long v_stride_tok,
@@ -489,12 +494,12 @@ evlnStatus_t evlnPaged8StepAttention(evlnHandle_t handle, const evlnPagedParams*
  *                         exp(softmax_scale q_ih . k_j - lse_ih),                                j = 0 .. L+n-1.
  * q_rot and k_cache as evlnRopeAppend leaves them, lse [n, Hq] as the step's combine writes it, params those of the step.
  * weights_in, weights_out float [Hkv, cache_capacity] (the same buffer, or two that do not overlap); slots from L+n on are not
- * touched, and weights_in is not read from slot L on.  decay >= 0.  bf16 and f32, head_dim 64 and 128.  num_splits
+ * touched, and weights_in is not read from slot L on.  decay >= 0, n >= 1.  bf16 and f32, head_dim 64 and 128.  num_splits
  * and kernel of params are not looked at.  Results do not depend on timing (no atomics).
  *
  * evlnSelectKeys: for each kv head the slots to keep of 0 .. num_keys-1: all of them where budget >= num_keys, else the first
  * `sinks`, the last `recent` and of those between the budget - sinks - recent of largest weight (equal weights: the
- * lower slot; NaN counts as less than any number).  kept [Hkv, min(budget, num_keys)] int, ascending.  weights
+ * lower slot; NaN counts as minus infinity).  kept [Hkv, min(budget, num_keys)] int, ascending.  weights
  * float [Hkv, store_capacity].  sinks + recent <= budget.
  *
  * evlnGatherKeys: the chosen slots of the store laid out back to back, kv head by kv head: key and value kept[g][p] of head g

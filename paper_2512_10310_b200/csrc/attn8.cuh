@@ -44,7 +44,7 @@ constexpr float kA8LeastGap = -90.f;                  // least v - r that is tol
 template <int NQ, int RG>
 struct Attn8Plan {
     // Twelve warps, three a scheduler that hide each other's chains.  (Eight of 255 registers with 32 rows each take 5 to 10 % less for large batches of
-    // 17 to 64 rows, 16 episodes of 8000 keys 86 us and 95, but more where latency counts, one of 4096 keys 14.5 and 12.5.)
+    // 17 to 64 rows, 16 episodes of 8000 keys 86 us and 95, but more where latency counts, one of 4096 keys 14.5 and 12.5; figures at the time.)
     static constexpr int kWarps = 12, kThreads = 32 * kWarps;
     static constexpr int kRegs = 168;
     static constexpr int kWarpRows = 8 * NQ, kRows = kWarpRows * RG;
@@ -521,7 +521,7 @@ struct MergeList {
 // of them in flight beside the references, before it is known what they weigh.
 // Blocks without such a unit leave at once (the first one does not: the next kernel in the stream waits for this grid, which
 // therefore must not end before the attention kernel has), so the others are on the SMs, and know what to read, when the parts are there.
-constexpr int kMergeAhead = 5;                         // (64 rows of one episode of 20656 keys: 25.5 us in all, with 3 26.4)
+constexpr int kMergeAhead = 5;                         // (with 3 64 rows of one episode of 20656 keys took 0.9 us longer)
 template <int ROWS> constexpr int kMergeWarps = ROWS >= 32 ? 8 : 4;            // (8 and 16 rows: few parts, many units)
 template <int ROWS, int KG>
 __global__ void __launch_bounds__(32 * kMergeWarps<ROWS>)

@@ -11,7 +11,7 @@
 // norm, rotation and the block's maximum to the codes: one pass.  Codes of earlier tokens are loaded instead of new ones and stored again only
 // if the scale grew.
 // Bound: latency for a token an episode (a chain of loads, the block's maximum, stores: 16 episodes 2.4 us), else the queries' traffic (16 frames of
-// 196 tokens with norms, 56 MB, 16.9 us).  (One token a lane, blocks of 512 threads: 2.7 and 21.4 us.)
+// 196 tokens with norms, 56 MB, 16.4 us).  (One token a lane, blocks of 512 threads: 2.7 and 21.4 us.)
 #pragma once
 
 #include <cuda_fp16.h>

@@ -156,8 +156,8 @@ void batch_lens(BatchLens* bl, const evlnPagedParams* p, const int* lens, const 
 // ---- attention over the cache in 8 bits ----------------------------------------------------------
 
 // Most query rows of an episode (per kv head) that the kernel on the codes serves: a block's.  More go through a bf16 copy, which takes the same time for
-// 70 rows as for 250, less than the codes twice.  (us, 63 rows on the codes, 70 and 252 through the copy: one episode of 4096 keys 13.3, 14.4 and
-// 16.6; of 20656 21.9, 27.4, 30.8; 16 of 8000 96, 121, 122.)
+// 70 rows as for 250, less than the codes twice.  (us, 63 rows on the codes, 70 and 252 through the copy: one episode of 4096 keys 14.4, 14.3 and
+// 16.4; of 20656 22.8, 27.5, 31.0; 16 of 8000 98, 121, 125.)
 constexpr int kA8MostRows = 64;
 
 struct Plan8 {

@@ -10,7 +10,8 @@
 // query chunks), warp 1 issues, warps 2 and 3 fetch the rows' log-sum-exps, warps 4-19 exponentiate: four groups of four (one warp per TMEM lane
 // quarter), two of which share a chunk of 128 rows, or which take whole tiles in turn where a tile is one chunk.  Score buffers: 4 x 128 columns.
 // Bound: many rows, the special-function unit (16 exponentials a cycle and SM; the products take a quarter of that); few
-// rows, reading the keys once.  (1372 rows of 4 kv heads over 4292 keys: 13.4 us, 5 of them exponentials; over 20196 46.4.  Two groups that fetched their
+// rows, reading the keys once.  (1372 rows of 4 kv heads over 4292 keys: 13.5 us with inputs out of DRAM, 11.3 with three sets of them in L2, 5.9 of them
+// exponentials; over 20196 46.4.  Two groups that fetched their
 // log-sum-exps themselves, and masked every block of a tile that some row does not see, took 15.3 and 58.8: a wait that has to poll costs 0.1 us,
 // a fetch 0.3 us.  Chunks of 64 rows are bound by the issuing warp, 17.9, of 256 have too few buffers, 14.5; a quarter to a half of the exponentials on the
 // FMA pipe, by a polynomial of degree 5: 13.9 to 14.4.  Per SM sub-partition, 32 scores of 32 keys take 360 cycles: 256 of exponentials, beside
